@@ -284,6 +284,195 @@ int fsched_simulate_noalloc(const fsched_params* p, int64_t n_inst, int32_t n_jo
                             const int32_t* output, fsched_metrics* out, int32_t* start,
                             int32_t* finish, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Operators of the step itself: what a worker runs for the requests that a
+ * schedule put into one step.  Requests hold their keys and values in pages of
+ * a KV cache; fsched_kv_layout gives the step's new tokens their places,
+ * fsched_qk_norm_rope puts keys and values there, and fsched_attend /
+ * fsched_attend_shared read them.
+ *
+ *   - Every array is a device pointer on the current device: flags must include
+ *     FSCHED_F_DEVICE_PTRS (EINVAL otherwise; a cache is never staged).  Calls
+ *     only enqueue work on `stream`; FSCHED_F_SYNC waits for it.  No other flag
+ *     is known (EINVAL).  Structs are host memory, read during the call.
+ *   - Lengths, tables, slots and positions are device data that the host does
+ *     not read.  Kernels check each index against its array: a length below 0
+ *     counts as 0, one beyond the block table's row as the row's capacity; a
+ *     page id outside 0 .. n_pages-1 holds no keys (what sits there is masked);
+ *     a slot outside the cache is not written.
+ *   - Elements are bf16 or f16; products accumulate and norms, softmax
+ *     statistics and rotations run in 32 bits.  Strides are in elements.  The
+ *     head dimension is contiguous; every other stride is a multiple of 8 and
+ *     every base pointer 16-byte aligned (EINVAL otherwise).
+ *   - At most FSCHED_MAX_REQ requests and FSCHED_MAX_STEP_TOKENS new tokens in a
+ *     step (ETOOLARGE).  Sizes of zero are valid and do nothing. */
+#define FSCHED_MAX_REQ 4096
+#define FSCHED_MAX_STEP_TOKENS (1 << 24)
+
+enum { FSCHED_BF16 = 0, FSCHED_F16 = 1 };
+
+/* A paged KV cache (88 bytes).  Element (page, head, slot, d) of the keys is at
+ * k[page * k_stride[0] + head * k_stride[1] + slot * k_stride[2] + d]; the values
+ * likewise.  Any order of page, head and slot is allowed (head before slot, the
+ * page of one head in one piece, reads fastest). */
+typedef struct {
+  void* k;
+  void* v;
+  int64_t k_stride[3], v_stride[3]; /* page, head, slot                          */
+  int32_t n_pages;                  /* >= 0                                      */
+  int32_t page_size;                /* tokens per page: a power of two, <= 65536 */
+  int32_t kv_heads;                 /* 1 .. 1024                                 */
+  int32_t head_dim;                 /* 64, 128 or 256 (ENOTIMPL otherwise)       */
+  int32_t dtype;                    /* FSCHED_BF16 | FSCHED_F16                  */
+  int32_t reserved;                 /* 0                                         */
+} fsched_kv_cache;
+
+/* fsched_kv_layout — places for the new tokens of a step.
+ *
+ * Request r holds old_len[r] tokens and gets new_len[r] more.  Its row of the
+ * block table lists the pages that hold its tokens in order; the pages it has
+ * are kept, and the ceil((old + new) / page_size) - ceil(old / page_size) more
+ * that it needs are taken from the front of free_pages, requests in order.
+ *   n_req, n_tok    requests; capacity of slots and positions (the host knows
+ *                   the step's tokens: sum of new_len)
+ *   page_size       as in fsched_kv_cache
+ *   table_width     entries of a row of the block table (its stride)
+ *   n_free          length of free_pages
+ *   first_pos       position of every request's first token (the length of a
+ *                   shared prefix, else 0)
+ *   flags           FSCHED_F_DEVICE_PTRS | FSCHED_F_SYNC
+ *   old_len, new_len  [n_req]
+ *   free_pages      [n_free] page ids
+ *   table           in/out [n_req][table_width]; only entries of new pages are
+ *                   written, so a repeated call gives the same table
+ *   slots           [n_tok] page * page_size + offset of every new token, the
+ *                   requests' tokens one after the other; -1 where the token has
+ *                   no page (beyond free_pages or the table row) and past the
+ *                   last token
+ *   positions       [n_tok] first_pos + old_len + index in the request; -1 past
+ *                   the last token
+ *   q_start         [n_req + 1] first token of every request (at most n_tok)
+ *   kv_len          [n_req] old + new
+ *   used            [2] new pages (those within the table rows) and new tokens in
+ *                   all.  More pages than n_free (the table then gets -1 for the
+ *                   missing ones) or more tokens than n_tok mean that the step
+ *                   does not fit.
+ * Slots are 32-bit: page_size times the largest page id below 2^31 (ids beyond
+ * give -1). */
+typedef struct {
+  int32_t n_req, n_tok, page_size, table_width, n_free, first_pos;
+  uint32_t flags;
+  int32_t reserved; /* 0 */
+} fsched_layout_params;
+
+int fsched_kv_layout(const fsched_layout_params* p, const int32_t* old_len,
+                     const int32_t* new_len, const int32_t* free_pages, int32_t* table,
+                     int32_t* slots, int32_t* positions, int32_t* q_start, int32_t* kv_len,
+                     int32_t* used, void* stream);
+
+/* fsched_qk_norm_rope — from the fused projection of a step's tokens to rotated
+ * queries and a filled cache, in one pass.
+ *
+ * Row t of qkv holds q_heads query heads, then kv_heads key heads, then kv_heads
+ * value heads.  Queries and keys are normed per head,
+ *   y = x / sqrt(mean(x^2) + eps) * weight,
+ * and their first rot_dim elements rotated in pairs (a, b) to
+ *   (a cos - b sin, b cos + a sin)
+ * with pairs (i, i + rot_dim/2), or (2i, 2i + 1) when `interleaved`; values are
+ * copied.  Queries go to q_out, keys and values to the slots of the cache; each
+ * is rounded once.
+ *   n_tok, q_heads  tokens; query heads, 1 .. 1024 (the cache gives kv_heads,
+ *                   head_dim and dtype)
+ *   rot_dim         a multiple of 16, 0 <= rot_dim <= head_dim
+ *   n_pos           rows of cos_sin
+ *   interleaved     0 | 1
+ *   eps             >= 0, finite
+ *   qkv_stride      elements from one token's row to the next (heads are
+ *                   head_dim apart)
+ *   q_token_stride, q_head_stride   strides of q_out
+ *   positions       [n_tok]; outside 0 .. n_pos-1 the token's queries are zero
+ *                   and nothing is stored (read only when rot_dim > 0)
+ *   slots           [n_tok] or NULL (nothing is stored); a slot outside the cache
+ *                   (-1) stores nothing.  Two tokens of one slot race.
+ *   cos_sin         [n_pos][rot_dim] f32, row = position: rot_dim/2 cosines, then
+ *                   the sines (NULL when rot_dim = 0)
+ *   q_weight, k_weight  [head_dim] of the cache's type, 16-byte aligned; NULL:
+ *                   that side is not normed
+ * q_out may be qkv's own query part (same strides). */
+typedef struct {
+  int32_t n_tok, q_heads, rot_dim, n_pos, interleaved;
+  float eps;
+  uint32_t flags;
+  int32_t reserved; /* 0 */
+  int64_t qkv_stride, q_token_stride, q_head_stride;
+} fsched_rope_params;
+
+int fsched_qk_norm_rope(const fsched_rope_params* p, const fsched_kv_cache* kv, const void* qkv,
+                        const int32_t* positions, const int32_t* slots, const float* cos_sin,
+                        const void* q_weight, const void* k_weight, void* q_out, void* stream);
+
+/* fsched_attend — attention of a step's new tokens over the paged cache.
+ *
+ * Token i of the q_r = q_start[r+1] - q_start[r] tokens of request r sits at
+ * position pos = kv_len[r] - q_r + i, the last of them at the end of what the
+ * request holds.  Query head h reads key head h / (q_heads / kv_heads).  It sees
+ * the keys j <= pos, with a window only those with j > pos - window or j < n_sink:
+ *   out = sum_j w_j v_j, w_j = exp(scale q.k_j - lse), lse = log sum_j exp(scale q.k_j).
+ * A token that sees no key (pos < 0, nothing held, pages masked) gets out = 0 and
+ * lse = -infinity.  What the cache holds in places that no token of a request
+ * sees (unwritten slots, pages past the window) does not matter, infinities and
+ * NaN included; keys and values that some token of the request sees are finite.
+ *   n_req, n_tok    requests and rows of q
+ *   q_heads         a multiple of kv_heads, at most 1024
+ *   max_q           no request has more new tokens than this (1 .. n_tok; it
+ *                   chooses the kernels: 1 for a decode step).  Tokens of a
+ *                   request past its first max_q are not computed: their rows of
+ *                   out and lse stay as they were.
+ *   table_width     entries of a row of the block table (its stride)
+ *   window          0: every earlier key is visible; else the last `window`
+ *   n_sink          first keys that stay visible behind a window
+ *   prefix_len      0 (fsched_attend_shared: see below)
+ *   scale           > 0, finite
+ *   q, out strides  token and head; out must not overlap q
+ *   table           [n_req][table_width] page ids; entries of pages that no token
+ *                   sees are not read
+ *   q_start         [n_req + 1] non-decreasing, within 0 .. n_tok
+ *   kv_len          [n_req]
+ *   lse             nullable [n_tok][q_heads] f32
+ *   workspace       device memory, 256-byte aligned, of at least the size that
+ *                   fsched_attend_workspace gives (ESCRATCH if smaller), whose
+ *                   contents need not be set and mean nothing after the call;
+ *                   calls that may overlap in time need one each.  NULL: taken from
+ *                   the library's pool (ENOMEM if it cannot be had).
+ * Results do not depend on the order in which the device runs the work: equal
+ * calls on one device give equal bits.
+ *
+ * fsched_attend_shared — the same for requests that all begin with one prefix of
+ * prefix_len tokens, whose keys and values are held once, in prefix_pages
+ * [ceil(prefix_len / page_size)], and read once for all requests.  kv_len and the
+ * block table describe each request's own tokens, which follow the prefix: token i
+ * sits at prefix_len + kv_len[r] - q_r + i. */
+typedef struct {
+  int32_t n_req, n_tok, q_heads, max_q, table_width, window, n_sink, prefix_len;
+  float scale;
+  uint32_t flags;
+  int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+} fsched_attn_params;
+
+int fsched_attend(const fsched_attn_params* p, const fsched_kv_cache* kv, const void* q,
+                  const int32_t* table, const int32_t* q_start, const int32_t* kv_len, void* out,
+                  float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+int fsched_attend_shared(const fsched_attn_params* p, const fsched_kv_cache* kv, const void* q,
+                         const int32_t* prefix_pages, const int32_t* table,
+                         const int32_t* q_start, const int32_t* kv_len, void* out, float* lse,
+                         void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that fsched_attend (or, with prefix_len > 0,
+ * fsched_attend_shared) of this shape uses on the current device; 0 is possible. */
+int fsched_attend_workspace(const fsched_attn_params* p, const fsched_kv_cache* kv,
+                            int64_t* bytes);
+
 /* Text for a return code (static storage). */
 const char* fsched_strerror(int code);
 

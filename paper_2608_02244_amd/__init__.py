@@ -37,7 +37,9 @@ METRICS_DTYPE = np.dtype([(f, np.int64) for f in METRIC_FIELDS[:12]] +
 METRICS_BYTES = 104
 EXPORTS = ("fsched_simulate", "fsched_simulate_robust", "fsched_cost_decompose", "fsched_bruteforce_opt",
            "fsched_strerror", "fsched_abi_version", "fsched_last_hip_error",
-           "fsched_release_cache", "fsched_simulate_noalloc")
+           "fsched_release_cache", "fsched_simulate_noalloc", "fsched_kv_layout",
+           "fsched_qk_norm_rope", "fsched_attend", "fsched_attend_shared",
+           "fsched_attend_workspace")
 
 
 class Params(ctypes.Structure):
@@ -73,6 +75,14 @@ def lib():
         L.fsched_simulate_robust.argtypes = [P, I64, I32, P, P, P, P, P, P, P, P]
         L.fsched_cost_decompose.argtypes = [P, I64, I32, P, P, P, P, P, P, P]
         L.fsched_bruteforce_opt.argtypes = [P, I64, I32, P, P, P, P, P, P]
+        L.fsched_kv_layout.argtypes = [P] * 11
+        L.fsched_qk_norm_rope.argtypes = [P] * 10
+        L.fsched_attend.argtypes = [P] * 9 + [I64, P]
+        L.fsched_attend_shared.argtypes = [P] * 10 + [I64, P]
+        L.fsched_attend_workspace.argtypes = [P] * 3
+        for f in (L.fsched_kv_layout, L.fsched_qk_norm_rope, L.fsched_attend,
+                  L.fsched_attend_shared, L.fsched_attend_workspace):
+            f.restype = ctypes.c_int
         for f in (L.fsched_simulate, L.fsched_simulate_noalloc, L.fsched_simulate_robust, L.fsched_cost_decompose, L.fsched_bruteforce_opt,
                   L.fsched_abi_version, L.fsched_last_hip_error, L.fsched_release_cache):
             f.restype = ctypes.c_int
@@ -285,6 +295,10 @@ def bruteforce_opt(arrival, prompt, output, *, B: int, alpha: int, M_kv: int = 0
     if rc:
         raise FschedError(rc, "fsched_bruteforce_opt")
     return T, st
+
+
+from .step import (attend, attend_shared, attend_workspace, kv_layout,  # noqa: E402,F401
+                   qk_norm_rope)
 
 
 def build():

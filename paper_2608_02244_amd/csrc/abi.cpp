@@ -298,22 +298,10 @@ int launch_simulate(const fsched_params* p, int64_t n_inst, int32_t n, const int
       ext_next += round256(bytes);
       return r;
     }
-    hipMemPool_t pool = rank_pool();
-    void* r = nullptr;
-    hipError_t e = pool ? hipMallocFromPoolAsync(&r, bytes, pool, s) : hipErrorNotSupported;
-    if (e != hipSuccess) {
-      (void)hipGetLastError();
-      r = nullptr;
-      e = hipMallocAsync(&r, bytes, s);
-    }
-    if (e != hipSuccess) {
-      (void)hipGetLastError();
-      return nullptr;
-    }
-    return r;
+    return fs::pool_alloc(bytes, s);
   };
   auto release = [&](void* r) {
-    if (!ext && r && hipFreeAsync(r, s) != hipSuccess) (void)hipGetLastError();
+    if (!ext) fs::pool_free(r, s);
   };
   a.rank_stride = Lay.rank_stride;
   a.rank = nullptr;
@@ -453,6 +441,28 @@ int check_simulate_args(const fsched_params* p, int64_t n_inst, int32_t n_jobs) 
 }
 
 int record_hip_error(hipError_t e) { return hip_fail(e); }
+
+int compute_units() { return device_cus(); }
+
+void* pool_alloc(size_t bytes, hipStream_t s) {
+  hipMemPool_t pool = rank_pool();
+  void* r = nullptr;
+  hipError_t e = pool ? hipMallocFromPoolAsync(&r, bytes, pool, s) : hipErrorNotSupported;
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    r = nullptr;
+    e = hipMallocAsync(&r, bytes, s);
+  }
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return nullptr;
+  }
+  return r;
+}
+
+void pool_free(void* ptr, hipStream_t s) {
+  if (ptr && hipFreeAsync(ptr, s) != hipSuccess) (void)hipGetLastError();
+}
 
 }  // namespace fs
 

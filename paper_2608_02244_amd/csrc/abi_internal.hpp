@@ -25,6 +25,14 @@ int simulate_with_scratch(const fsched_params* p, int64_t n_inst, int32_t n_jobs
 // Parameter and size checks of fsched_simulate.
 int check_simulate_args(const fsched_params* p, int64_t n_inst, int32_t n_jobs);
 
+// Compute units of the current device, 0 if the runtime cannot tell.
+int compute_units();
+
+// Scratch of a call: stream-ordered, from the library's pool (else the device's
+// default pool); null if neither has it.
+void* pool_alloc(size_t bytes, hipStream_t stream);
+void pool_free(void* ptr, hipStream_t stream);
+
 // Keep e as the thread's last HIP error and map it to a return code.
 int record_hip_error(hipError_t e);
 

@@ -1,0 +1,172 @@
+// Places for the new tokens of a step: block tables, slot maps, positions
+// (fsched_kv_layout).
+//
+// With need_r = ceil((old_r + new_r) / P) and have_r = ceil(old_r / P), request r
+// takes the need_r - have_r pages after those of the requests before it: two
+// prefix sums over the requests (pages and tokens) say everything, and each
+// token and each new page then finds its request by bisection.
+//
+// One launch: every block sums over all requests itself (at most 4,096 lengths,
+// 32 KiB from L2) rather than wait for a launch that does it once, then takes
+// its share of tokens, pages and requests.  A token reads its page from the
+// table only where the page was there before, else from the free list, so that
+// nothing written in the launch is read in it.
+#include <hip/hip_runtime.h>
+
+#include <climits>
+
+#include "step_common.hpp"
+
+namespace fs {
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int MAX_REQ = FSCHED_MAX_REQ;
+constexpr int TOK = 4;  // tokens per thread and turn: one 16-byte store each
+
+__device__ __forceinline__ int32_t sat32(int64_t x) {
+  return x > INT_MAX ? INT_MAX : (int32_t)x;
+}
+
+// Inclusive sums of x over the block's threads (in thread order).
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* wave_sum) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  if (lane == 63) wave_sum[wave] = x;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) x += wave_sum[w];
+  __syncthreads();
+  return x;
+}
+
+// Last r with start[r] <= x (start[0] = 0 <= x); requests without an element of
+// their own are passed over.
+__device__ __forceinline__ int find(const int32_t* start, int n, int x) {
+  int lo = 0, hi = n;  // start[lo] <= x < start[hi] (start[n] is the total)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (start[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(THREADS) void kv_layout_kernel(LayoutArgs a) {
+  __shared__ int32_t tok0[MAX_REQ + 1], page0[MAX_REQ + 1];
+  __shared__ int64_t wave_sum[THREADS / 64];
+  const int n = a.n_req;
+  const int per = (n + THREADS - 1) / THREADS;
+  const int r0 = min(n, (int)threadIdx.x * per), r1 = min(n, r0 + per);
+  const int shift = a.page_shift;
+  const int64_t page = 1ll << shift;
+
+  auto lens = [&](int r, int64_t* old_len, int64_t* add) {
+    *old_len = max(0, a.old_len[r]);
+    *add = max(0, a.new_len[r]);
+  };
+  // pages of the first `len` tokens, as far as the table row goes
+  auto pages_of = [&](int64_t len) { return min((len + page - 1) >> shift, (int64_t)a.width); };
+
+  int64_t toks = 0, pages = 0;
+  for (int r = r0; r < r1; ++r) {
+    int64_t o, m;
+    lens(r, &o, &m);
+    toks += m;
+    pages += pages_of(o + m) - pages_of(o);
+  }
+  int64_t t = block_scan(toks, wave_sum) - toks;
+  int64_t g = block_scan(pages, wave_sum) - pages;
+  for (int r = r0; r < r1; ++r) {
+    int64_t o, m;
+    lens(r, &o, &m);
+    tok0[r] = sat32(t);
+    page0[r] = sat32(g);
+    t += m;
+    g += pages_of(o + m) - pages_of(o);
+  }
+  // the last thread holds the totals (its range may be empty)
+  if (threadIdx.x == THREADS - 1) {
+    tok0[n] = sat32(t);
+    page0[n] = sat32(g);
+  }
+  __syncthreads();
+  const int all_tok = tok0[n], all_pages = page0[n];
+  const int id = blockIdx.x * THREADS + threadIdx.x, step = gridDim.x * THREADS;
+
+  for (int r = id; r <= n; r += step) {
+    a.q_start[r] = min(tok0[r], a.n_tok);
+    if (r < n) {
+      int64_t o, m;
+      lens(r, &o, &m);
+      a.kv_len[r] = sat32(o + m);
+    }
+  }
+  if (id == 0) {
+    a.used[0] = all_pages;
+    a.used[1] = all_tok;
+  }
+
+  // new pages: entry c of row r is free page page0[r] + c - have
+  for (int64_t i = id; i < all_pages; i += step) {
+    const int r = find(page0, n, (int)i);
+    const int64_t c = pages_of(max(0, a.old_len[r])) + (i - page0[r]);
+    if (c < a.width) a.table[(int64_t)r * a.width + c] = i < a.n_free ? a.free_pages[i] : -1;
+  }
+
+  const int limit = min(all_tok, a.n_tok);
+  const bool wide = (((uintptr_t)a.slots | (uintptr_t)a.positions) & 15) == 0;
+  for (int64_t base = (int64_t)id * TOK; base < a.n_tok; base += (int64_t)step * TOK) {
+    int32_t slot[TOK], pos[TOK];
+    int r = base < limit ? find(tok0, n, (int)base) : n;
+#pragma unroll
+    for (int j = 0; j < TOK; ++j) {
+      const int i = (int)base + j;
+      slot[j] = pos[j] = -1;
+      if (i >= limit) continue;
+      while (tok0[r + 1] <= i) ++r;
+      const int64_t o = max(0, a.old_len[r]);
+      const int64_t at = o + (i - tok0[r]);  // index in the request
+      const int64_t c = at >> shift, have = pages_of(o);
+      pos[j] = sat32(at + a.first_pos);
+      if (c >= a.width) continue;
+      int32_t id_page = -1;
+      if (c < have) {
+        id_page = a.table[(int64_t)r * a.width + c];
+      } else {
+        const int64_t f = page0[r] + (c - have);
+        if (f < a.n_free) id_page = a.free_pages[f];
+      }
+      const int64_t s = ((int64_t)id_page << shift) + (at & (page - 1));
+      if (id_page >= 0 && s <= INT_MAX) slot[j] = (int32_t)s;
+    }
+    const int left = a.n_tok - (int)base;
+    if (wide && left >= TOK) {
+      *(int4*)(a.slots + base) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+      *(int4*)(a.positions + base) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < TOK; ++j) {
+        if (j >= left) break;
+        a.slots[base + j] = slot[j];
+        a.positions[base + j] = pos[j];
+      }
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_kv_layout(const LayoutArgs& a, hipStream_t s) {
+  const int64_t per = THREADS * TOK;
+  int64_t blocks = ((int64_t)a.n_tok + per - 1) / per;
+  if (blocks < 1) blocks = 1;
+  if (blocks > 2048) blocks = 2048;
+  kv_layout_kernel<<<dim3((unsigned)blocks), dim3(THREADS), 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace fs
