@@ -1,105 +1,237 @@
 // Attention of a step's new tokens over the paged cache (fsched_attend,
-// fsched_attend_shared): one wave per token and query head, one pass over the
-// keys with the running maximum and sum of the softmax.
+// fsched_attend_shared): which kernels a call runs, and the joining of parts.
+//
+//   rows kernel   requests with few rows (tokens times query heads per key head):
+//                 bound by the bytes of the cache
+//   tiles kernel  requests with many rows, and all tokens' rows over a shared prefix:
+//                 bound by the products
+//   join          where a result came in parts: a request's keys cut over blocks, or
+//                 prefix and own keys
 #include <hip/hip_runtime.h>
 
-#include "half.hpp"
-#include "step_common.hpp"
+#include "attend_common.hpp"
+#include "attend_rows.hpp"
+#include "attend_tiles.hpp"
 
 namespace fs {
 namespace {
 
-constexpr float NEG = -INFINITY;
+constexpr int THREADS = 256;
 
+struct JoinArgs {
+  int row_limit;  // rows of a request in the rows kernel's parts (16 per row tile), 0: none ran
+  int own_split;  // parts of the tiles kernel over own keys, 0: none (or results)
+  int pre_split;  // parts over the prefix, 0: no prefix
+  const float* rows_o;
+  const float2* rows_ml;
+  const RowsTile* tiles;
+  const float* own_o;
+  const float2* own_ml;
+  const float* pre_o;
+  const float2* pre_ml;
+};
+
+// Running join of parts of one row, 8 elements of it.
+struct Joined {
+  float m = NEG_INF, l = 0.0f, o[8] = {};
+  __device__ __forceinline__ void add(float2 ml, const float* src) {
+    if (ml.x == NEG_INF) return;
+    const float to = fmaxf(m, ml.x);
+    const float f = part_scale(m, to), g = exp2_fast(ml.x - to);
+    const f32x4 y = *(const f32x4*)src, z = *(const f32x4*)(src + 4);
+    m = to;
+    l = l * f + ml.y * g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[i] = o[i] * f + y[i] * g;
+      o[4 + i] = o[4 + i] * f + z[i] * g;
+    }
+  }
+};
+
+// One block per request, key head and group of ROWS rows; D/8 threads hold a row,
+// and where there are fewer rows than that fills, several such groups share its parts.
 template <class T, int D>
-__global__ __launch_bounds__(64) void attend_simple(AttnArgs a) {
-  constexpr int LANES = D / 8, KEYS = 64 / LANES;
+__global__ __launch_bounds__(THREADS) void attend_join_kernel(AttnArgs a, JoinArgs j) {
+  constexpr int LANES = D / 8, GROUPS = THREADS / LANES;
   using elem = typename T::elem;
   using x8 = typename T::x8;
-  const int lane = threadIdx.x, sub = lane & (LANES - 1), grp = lane / LANES;
-  const int h = blockIdx.x % a.q_heads;
-  const int t = blockIdx.x / a.q_heads;
-  int lo = 0, hi = a.n_req;  // last request with q_start <= t
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.q_start[mid] <= t) lo = mid;
-    else hi = mid;
-  }
-  const int r = lo;
-  const int q0 = max(0, a.q_start[r]), q1 = min(a.n_tok, a.q_start[r + 1]);
-  if (t < q0 || t >= q1 || t - q0 >= a.max_q) return;
-  const int own = min(max(0, a.kv_len[r]), a.width << a.kv.page_shift);
-  const int pos = a.prefix_len + own - (q1 - q0) + (t - q0);
-  const int total = min(a.prefix_len + own, pos + 1);
-  const int kh = h / a.group;
-  const int mask = (1 << a.kv.page_shift) - 1;
+  __shared__ float other[GROUPS][D + 4];
+  __shared__ float2 other_ml[GROUPS];
+  const int r = blockIdx.x % a.n_req, kh = blockIdx.x / a.n_req;
+  const Request x = request_of(a, r);
+  const int rows = min(x.q_len, a.max_q) * a.group;
+  if (rows == 0) return;
+  const bool few = rows <= j.row_limit;
+  RowsTile t = {0, 0, 0, 0};
+  if (few) t = j.tiles[(int64_t)kh * a.n_req + r];
+  const int own = few ? t.count : j.own_split;
+  if (j.pre_split == 0 && (few ? own <= 1 : own == 0)) return;  // written already
 
-  float q[8];
-  const x8 qr = *(const x8*)((const elem*)a.q + t * a.q_token + h * a.q_head + sub * 8);
+  const int grp = threadIdx.x / LANES, d0 = (threadIdx.x % LANES) * 8;
+  int at_once = 1;  // rows at once; GROUPS / at_once groups share one
+  while (at_once < rows && at_once < GROUPS) at_once *= 2;
+  const int share = GROUPS / at_once, mine = grp / at_once, sub = grp % at_once;
+  const int parts = own + j.pre_split;
+  for (int base = blockIdx.y * at_once; base < rows; base += gridDim.y * at_once) {
+    const int row = base + sub;
+    const bool on = row < rows;
+    const int tok = x.q0 + (on ? row / a.group : 0);
+    const int qh = kh * a.group + (on ? row % a.group : 0);
+    const int64_t th = (int64_t)tok * a.q_heads + qh, all = (int64_t)a.n_tok * a.q_heads;
+    Joined s;
+    if (on) {
+      for (int i = mine; i < parts; i += share) {
+        if (i >= own) {
+          const int64_t at = (int64_t)(i - own) * all + th;
+          s.add(j.pre_ml[at], j.pre_o + at * D + d0);
+        } else if (few) {
+          const int64_t slot = i == 0 ? t.first : 2 * ((int64_t)t.block + i);
+          const int64_t at = slot * j.row_limit + row;
+          s.add(j.rows_ml[at], j.rows_o + at * D + d0);
+        } else {
+          const int64_t at = (int64_t)i * all + th;
+          s.add(j.own_ml[at], j.own_o + at * D + d0);
+        }
+      }
+    }
+    if (share > 1) {
+      __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = (float)qr[i] * a.scale_log2;
-  float m = NEG, l = 0.0f, o[8] = {};
-  for (int j = grp; j < total; j += KEYS) {
-    const bool in_window = a.window == 0 || j > pos - a.window || j < a.n_sink;
-    if (!in_window) continue;
-    const bool pre = j < a.prefix_len;
-    const int x = pre ? j : j - a.prefix_len;
-    const int page = pre ? a.prefix_pages[x >> a.kv.page_shift]
-                         : a.table[(int64_t)r * a.width + (x >> a.kv.page_shift)];
-    if (page < 0 || page >= a.kv.n_pages) continue;
-    const x8 kr = *(const x8*)((const elem*)a.kv.k + page * a.kv.k_page + kh * a.kv.k_head +
-                               (x & mask) * a.kv.k_slot + sub * 8);
-    const x8 vr = *(const x8*)((const elem*)a.kv.v + page * a.kv.v_page + kh * a.kv.v_head +
-                               (x & mask) * a.kv.v_slot + sub * 8);
-    float s = 0.0f;
+      for (int i = 0; i < 8; i += 4)
+        *(f32x4*)&other[grp][d0 + i] = (f32x4){s.o[i], s.o[i + 1], s.o[i + 2], s.o[i + 3]};
+      if (d0 == 0) other_ml[grp] = make_float2(s.m, s.l);
+      __syncthreads();
+      if (mine == 0)
+        for (int i = 1; i < share; ++i)
+          s.add(other_ml[i * at_once + sub], &other[i * at_once + sub][d0]);
+    }
+    if (mine == 0 && on) {
+      const float inv = s.l > 0.0f ? 1.0f / s.l : s.l == 0.0f ? 0.0f : s.l;
+      x8 out;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s = fmaf(q[i], (float)kr[i], s);
-#pragma unroll
-    for (int d = 1; d < LANES; d <<= 1) s += __shfl_xor(s, d);
-    const float m2 = fmaxf(m, s);
-    const float f = m2 == NEG ? 1.0f : exp2f(m - m2), p = m2 == NEG ? 0.0f : exp2f(s - m2);
-    m = m2;
-    l = l * f + p;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = o[i] * f + p * (float)vr[i];
-  }
-#pragma unroll
-  for (int d = LANES; d < 64; d <<= 1) {
-    const float mo = __shfl_xor(m, d), lo2 = __shfl_xor(l, d);
-    const float m2 = fmaxf(m, mo);
-    const float f = m == NEG ? 0.0f : exp2f(m - m2), g = mo == NEG ? 0.0f : exp2f(mo - m2);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = o[i] * f + __shfl_xor(o[i], d) * g;
-    l = l * f + lo2 * g;
-    m = m2;
-  }
-  if (grp == 0) {
-    x8 res;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) res[i] = (elem)(l > 0.0f ? o[i] / l : 0.0f);
-    *(x8*)((elem*)a.out + t * a.o_token + h * a.o_head + sub * 8) = res;
-    if (a.lse && sub == 0)
-      a.lse[(int64_t)t * a.q_heads + h] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : NEG;
+      for (int i = 0; i < 8; ++i) out[i] = (elem)(s.o[i] * inv);
+      *(x8*)((elem*)a.out + (int64_t)tok * a.o_token + (int64_t)qh * a.o_head + d0) = out;
+      if (a.lse && d0 == 0) a.lse[th] = (s.m + log2f(s.l)) * LN2;
+    }
   }
 }
 
-template <class T>
-hipError_t launch(const AttnArgs& a, int head_dim, hipStream_t s) {
-  const dim3 grid((unsigned)(a.n_tok * a.q_heads));
-  switch (head_dim) {
-    case 64: attend_simple<T, 64><<<grid, 64, 0, s>>>(a); break;
-    case 128: attend_simple<T, 128><<<grid, 64, 0, s>>>(a); break;
-    default: attend_simple<T, 256><<<grid, 64, 0, s>>>(a); break;
+// What a call of this shape launches, and where its workspace's parts lie.
+struct Shape {
+  bool rows, tiles;    // kernels over own keys
+  RowsPlan rp;
+  TilesPlan own, pre;
+  JoinArgs join;
+  bool joins;
+  size_t bytes;
+};
+
+size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+Shape plan(const AttnArgs& a, int head_dim, int n_cu, char* ws) {
+  Shape p;
+  __builtin_memset((void*)&p, 0, sizeof(p));
+  if (n_cu <= 0) n_cu = 256;
+  size_t used = 0;
+  auto take = [&](size_t bytes) {
+    char* at = ws + used;
+    used += round256(bytes);
+    return ws ? at : nullptr;
+  };
+  const int64_t th = (int64_t)a.n_tok * a.q_heads;
+  const int64_t rows = (int64_t)a.n_tok * a.group;            // rows of a key head
+  const int64_t most = (int64_t)a.max_q * a.group;            // of one request, at most
+  const bool prefix = a.prefix_len > 0;
+
+  // The rows kernel holds 16 or 32 rows (16 where a head's registers are many).
+  const int held = head_dim == 256 ? 16 : 32;
+  p.rows = a.group <= held;
+  p.tiles = most > held;
+  p.rp.row_tiles = a.group > 16 || (most > 16 && most <= held) ? 2 : 1;
+  const int limit = p.rows ? 16 * p.rp.row_tiles : 0;
+  if (p.rows) {
+    p.rp.blocks = rows_blocks(head_dim, p.rp.row_tiles, n_cu);
+    p.rp.keep_parts = prefix;
+    const size_t slots = 2 * (size_t)p.rp.blocks * limit;
+    p.rp.part_o = (float*)take(slots * head_dim * sizeof(float));
+    p.rp.part_ml = (float2*)take(slots * sizeof(float2));
+    p.rp.tiles = (RowsTile*)take((size_t)a.n_req * a.kv.kv_heads * sizeof(RowsTile));
+    p.join.row_limit = limit;
+    p.join.rows_o = p.rp.part_o;
+    p.join.rows_ml = p.rp.part_ml;
+    p.join.tiles = p.rp.tiles;
   }
-  return hipGetLastError();
+  // Keys are cut so that about two blocks per compute unit have work, none with
+  // fewer than 256 keys.
+  auto cut = [&](int64_t tiles, int64_t keys) {
+    const int64_t want = (2 * (int64_t)n_cu + tiles * a.kv.kv_heads - 1) / (tiles * a.kv.kv_heads);
+    const int64_t can = keys / 256 > 1 ? keys / 256 : 1;
+    const int64_t s = want < can ? want : can;
+    return (int)(s < 1 ? 1 : s);
+  };
+  if (p.tiles) {
+    // requests that are not the rows kernel's have more than `limit` rows each
+    const int64_t big = rows / (limit + 1);
+    p.own.tiles = (int)(rows / TILE_ROWS + (big < a.n_req ? big : a.n_req));
+    if (p.own.tiles < 1) p.own.tiles = 1;
+    p.own.min_rows = limit;
+    p.own.split = cut(p.own.tiles, (int64_t)a.width << a.kv.page_shift);
+    p.own.parts = prefix || p.own.split > 1;
+    if (p.own.parts) {
+      p.own.part_o = (float*)take((size_t)p.own.split * th * head_dim * sizeof(float));
+      p.own.part_ml = (float2*)take((size_t)p.own.split * th * sizeof(float2));
+      p.join.own_split = p.own.split;
+      p.join.own_o = p.own.part_o;
+      p.join.own_ml = p.own.part_ml;
+    }
+  }
+  if (prefix) {
+    p.pre.prefix = 1;
+    p.pre.tiles = (int)((rows + TILE_ROWS - 1) / TILE_ROWS);
+    p.pre.split = cut(p.pre.tiles, a.prefix_len);
+    p.pre.parts = 1;
+    p.pre.part_o = (float*)take((size_t)p.pre.split * th * head_dim * sizeof(float));
+    p.pre.part_ml = (float2*)take((size_t)p.pre.split * th * sizeof(float2));
+    p.join.pre_split = p.pre.split;
+    p.join.pre_o = p.pre.part_o;
+    p.join.pre_ml = p.pre.part_ml;
+  }
+  p.joins = p.rows || p.join.own_split || prefix;
+  p.bytes = used;
+  return p;
+}
+
+template <class T>
+void join(const AttnArgs& a, const JoinArgs& j, int head_dim, dim3 grid, hipStream_t s) {
+  switch (head_dim) {
+    case 64: attend_join_kernel<T, 64><<<grid, THREADS, 0, s>>>(a, j); break;
+    case 128: attend_join_kernel<T, 128><<<grid, THREADS, 0, s>>>(a, j); break;
+    default: attend_join_kernel<T, 256><<<grid, THREADS, 0, s>>>(a, j); break;
+  }
 }
 
 }  // namespace
 
-size_t attend_workspace(const AttnArgs&, int, int, int) { return 0; }
+size_t attend_workspace(const AttnArgs& a, int, int head_dim, int n_cu) {
+  return plan(a, head_dim, n_cu, nullptr).bytes;
+}
 
-hipError_t launch_attend(const AttnArgs& a, int dtype, int head_dim, int, void*, hipStream_t s) {
-  return dtype == FSCHED_BF16 ? launch<Bf16>(a, head_dim, s) : launch<F16>(a, head_dim, s);
+hipError_t launch_attend(const AttnArgs& a, int dtype, int head_dim, int n_cu, void* workspace,
+                         hipStream_t s) {
+  const Shape p = plan(a, head_dim, n_cu, (char*)workspace);
+  hipError_t e = hipSuccess;
+  if (a.prefix_len > 0) e = launch_attend_tiles(a, p.pre, dtype, head_dim, s);
+  if (e == hipSuccess && p.tiles) e = launch_attend_tiles(a, p.own, dtype, head_dim, s);
+  if (e == hipSuccess && p.rows) e = launch_attend_rows(a, p.rp, dtype, head_dim, s);
+  if (e != hipSuccess || !p.joins) return e;
+  // requests with many rows: more blocks per request
+  const int64_t most = (int64_t)a.max_q * a.group;
+  const unsigned y = (unsigned)(most <= 64 ? 1 : most / 64 < 256 ? most / 64 : 256);
+  const dim3 grid((unsigned)(a.n_req * a.kv.kv_heads), y);
+  if (dtype == FSCHED_BF16) join<Bf16>(a, p.join, head_dim, grid, s);
+  else join<F16>(a, p.join, head_dim, grid, s);
+  return hipGetLastError();
 }
 
 }  // namespace fs
