@@ -297,8 +297,16 @@ def bruteforce_opt(arrival, prompt, output, *, B: int, alpha: int, M_kv: int = 0
     return T, st
 
 
-from .step import (attend, attend_shared, attend_workspace, kv_layout,  # noqa: E402,F401
-                   qk_norm_rope)
+_STEP = ("attend", "attend_shared", "attend_workspace", "kv_layout", "qk_norm_rope")
+
+
+def __getattr__(name):
+    """The step operators (module ``step``), loaded with torch on their first use."""
+    if name in _STEP:
+        from . import step
+        globals().update((n, getattr(step, n)) for n in _STEP)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def build():
