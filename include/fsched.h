@@ -314,7 +314,8 @@ enum { FSCHED_BF16 = 0, FSCHED_F16 = 1 };
 /* A paged KV cache (88 bytes).  Element (page, head, slot, d) of the keys is at
  * k[page * k_stride[0] + head * k_stride[1] + slot * k_stride[2] + d]; the values
  * likewise.  Any order of page, head and slot is allowed (head before slot, the
- * page of one head in one piece, reads fastest). */
+ * page of one head in one piece, reads fastest); the slots of a page span at most
+ * 2^27 elements and no stride exceeds 2^40 (ETOOLARGE). */
 typedef struct {
   void* k;
   void* v;

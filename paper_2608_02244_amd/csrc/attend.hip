@@ -1,17 +1,15 @@
 // Attention of a step's new tokens over the paged cache (fsched_attend,
 // fsched_attend_shared): which kernels a call runs, and the joining of parts.
 //
-//   rows kernel   requests with few rows (tokens times query heads per key head):
+//   rows blocks   requests with few rows (tokens times query heads per key head):
 //                 bound by the bytes of the cache
-//   tiles kernel  requests with many rows, and all tokens' rows over a shared prefix:
+//   tiles blocks  requests with many rows, and all tokens' rows over a shared prefix:
 //                 bound by the products
-//   join          where a result came in parts: a request's keys cut over blocks, or
-//                 prefix and own keys
+//   join          a second launch, where results came in parts: a request's keys cut
+//                 over waves or blocks, or a prefix and own keys
 #include <hip/hip_runtime.h>
 
-#include "attend_common.hpp"
-#include "attend_rows.hpp"
-#include "attend_tiles.hpp"
+#include "attend_main.hpp"
 
 namespace fs {
 namespace {
@@ -19,7 +17,8 @@ namespace {
 constexpr int THREADS = 256;
 
 struct JoinArgs {
-  int row_limit;  // rows of a request in the rows kernel's parts (16 per row tile), 0: none ran
+  int row_limit;  // requests with at most this many rows were the rows kernel's, 0: none
+  int slot_rows;  // rows of a slot of its parts
   int own_split;  // parts of the tiles kernel over own keys, 0: none (or results)
   int pre_split;  // parts over the prefix, 0: no prefix
   const float* rows_o;
@@ -86,8 +85,8 @@ __global__ __launch_bounds__(THREADS) void attend_join_kernel(AttnArgs a, JoinAr
           const int64_t at = (int64_t)(i - own) * all + th;
           s.add(j.pre_ml[at], j.pre_o + at * D + d0);
         } else if (few) {
-          const int64_t slot = i == 0 ? t.first : 2 * ((int64_t)t.block + i);
-          const int64_t at = slot * j.row_limit + row;
+          const int64_t slot = i == 0 ? t.first : 2 * ((int64_t)t.wave + i);
+          const int64_t at = slot * j.slot_rows + row;
           s.add(j.rows_ml[at], j.rows_o + at * D + d0);
         } else {
           const int64_t at = (int64_t)i * all + th;
@@ -119,9 +118,7 @@ __global__ __launch_bounds__(THREADS) void attend_join_kernel(AttnArgs a, JoinAr
 
 // What a call of this shape launches, and where its workspace's parts lie.
 struct Shape {
-  bool rows, tiles;    // kernels over own keys
-  RowsPlan rp;
-  TilesPlan own, pre;
+  MainPlan main;
   JoinArgs join;
   bool joins;
   size_t bytes;
@@ -146,21 +143,28 @@ Shape plan(const AttnArgs& a, int head_dim, int n_cu, char* ws) {
 
   // The rows kernel holds 16 or 32 rows (16 where a head's registers are many).
   const int held = head_dim == 256 ? 16 : 32;
-  p.rows = a.group <= held;
-  p.tiles = most > held;
-  p.rp.row_tiles = a.group > 16 || (most > 16 && most <= held) ? 2 : 1;
-  const int limit = p.rows ? 16 * p.rp.row_tiles : 0;
-  if (p.rows) {
-    p.rp.blocks = rows_blocks(head_dim, p.rp.row_tiles, n_cu);
-    p.rp.keep_parts = prefix;
-    const size_t slots = 2 * (size_t)p.rp.blocks * limit;
-    p.rp.part_o = (float*)take(slots * head_dim * sizeof(float));
-    p.rp.part_ml = (float2*)take(slots * sizeof(float2));
-    p.rp.tiles = (RowsTile*)take((size_t)a.n_req * a.kv.kv_heads * sizeof(RowsTile));
+  const bool with_rows = a.group <= held, with_tiles = most > held;
+  RowsPlan& rp = p.main.rows;
+  rp.row_tiles = a.group > 16 || (most > 16 && most <= held) ? 2 : 1;
+  const int limit = with_rows ? 16 * rp.row_tiles : 0;
+  if (with_rows) {
+    // beside tiles blocks one rows block per compute unit, else as many as fit
+    p.main.rows_blocks = with_tiles || prefix
+                             ? n_cu
+                             : n_cu * rows_occupancy(head_dim, rp.row_tiles,
+                                                     a.kv.page_shift >= WIDE_SHIFT);
+    rp.waves = p.main.rows_blocks * ATT_WAVES;
+    rp.keep_parts = prefix;
+    rp.slot_rows = most < limit ? (int)most : limit;
+    const size_t slots = 2 * (size_t)rp.waves * rp.slot_rows;
+    rp.part_o = (float*)take(slots * head_dim * sizeof(float));
+    rp.part_ml = (float2*)take(slots * sizeof(float2));
+    rp.tiles = (RowsTile*)take((size_t)a.n_req * a.kv.kv_heads * sizeof(RowsTile));
     p.join.row_limit = limit;
-    p.join.rows_o = p.rp.part_o;
-    p.join.rows_ml = p.rp.part_ml;
-    p.join.tiles = p.rp.tiles;
+    p.join.slot_rows = rp.slot_rows;
+    p.join.rows_o = rp.part_o;
+    p.join.rows_ml = rp.part_ml;
+    p.join.tiles = rp.tiles;
   }
   // Keys are cut so that about two blocks per compute unit have work, none with
   // fewer than 256 keys.
@@ -170,36 +174,48 @@ Shape plan(const AttnArgs& a, int head_dim, int n_cu, char* ws) {
     const int64_t s = want < can ? want : can;
     return (int)(s < 1 ? 1 : s);
   };
-  if (p.tiles) {
+  if (with_tiles) {
+    TilesPlan& t = p.main.own;
     // requests that are not the rows kernel's have more than `limit` rows each
     const int64_t big = rows / (limit + 1);
-    p.own.tiles = (int)(rows / TILE_ROWS + (big < a.n_req ? big : a.n_req));
-    if (p.own.tiles < 1) p.own.tiles = 1;
-    p.own.min_rows = limit;
-    p.own.split = cut(p.own.tiles, (int64_t)a.width << a.kv.page_shift);
-    p.own.parts = prefix || p.own.split > 1;
-    if (p.own.parts) {
-      p.own.part_o = (float*)take((size_t)p.own.split * th * head_dim * sizeof(float));
-      p.own.part_ml = (float2*)take((size_t)p.own.split * th * sizeof(float2));
-      p.join.own_split = p.own.split;
-      p.join.own_o = p.own.part_o;
-      p.join.own_ml = p.own.part_ml;
+    const int64_t tiles = rows / TILE_ROWS + (big < a.n_req ? big : a.n_req);
+    t.min_rows = limit;
+    t.split = cut(tiles < 1 ? 1 : tiles, (int64_t)a.width << a.kv.page_shift);
+    t.parts = prefix || t.split > 1;
+    p.main.own_blocks = (int)((tiles < 1 ? 1 : tiles) * t.split * a.kv.kv_heads);
+    if (t.parts) {
+      t.part_o = (float*)take((size_t)t.split * th * head_dim * sizeof(float));
+      t.part_ml = (float2*)take((size_t)t.split * th * sizeof(float2));
+      p.join.own_split = t.split;
+      p.join.own_o = t.part_o;
+      p.join.own_ml = t.part_ml;
     }
   }
   if (prefix) {
-    p.pre.prefix = 1;
-    p.pre.tiles = (int)((rows + TILE_ROWS - 1) / TILE_ROWS);
-    p.pre.split = cut(p.pre.tiles, a.prefix_len);
-    p.pre.parts = 1;
-    p.pre.part_o = (float*)take((size_t)p.pre.split * th * head_dim * sizeof(float));
-    p.pre.part_ml = (float2*)take((size_t)p.pre.split * th * sizeof(float2));
-    p.join.pre_split = p.pre.split;
-    p.join.pre_o = p.pre.part_o;
-    p.join.pre_ml = p.pre.part_ml;
+    TilesPlan& t = p.main.pre;
+    const int64_t tiles = (rows + TILE_ROWS - 1) / TILE_ROWS;
+    t.prefix = 1;
+    t.split = cut(tiles, a.prefix_len);
+    t.parts = 1;
+    p.main.pre_blocks = (int)(tiles * t.split * a.kv.kv_heads);
+    t.part_o = (float*)take((size_t)t.split * th * head_dim * sizeof(float));
+    t.part_ml = (float2*)take((size_t)t.split * th * sizeof(float2));
+    p.join.pre_split = t.split;
+    p.join.pre_o = t.part_o;
+    p.join.pre_ml = t.part_ml;
   }
-  p.joins = p.rows || p.join.own_split || prefix;
+  p.joins = with_rows || p.join.own_split || prefix;
   p.bytes = used;
   return p;
+}
+
+template <class T>
+hipError_t main_launch(const AttnArgs& a, const MainPlan& p, int head_dim, hipStream_t s) {
+  switch (head_dim) {
+    case 64: return launch_main<T, 64>(a, p, s);
+    case 128: return launch_main<T, 128>(a, p, s);
+    default: return launch_main<T, 256>(a, p, s);
+  }
 }
 
 template <class T>
@@ -220,10 +236,8 @@ size_t attend_workspace(const AttnArgs& a, int, int head_dim, int n_cu) {
 hipError_t launch_attend(const AttnArgs& a, int dtype, int head_dim, int n_cu, void* workspace,
                          hipStream_t s) {
   const Shape p = plan(a, head_dim, n_cu, (char*)workspace);
-  hipError_t e = hipSuccess;
-  if (a.prefix_len > 0) e = launch_attend_tiles(a, p.pre, dtype, head_dim, s);
-  if (e == hipSuccess && p.tiles) e = launch_attend_tiles(a, p.own, dtype, head_dim, s);
-  if (e == hipSuccess && p.rows) e = launch_attend_rows(a, p.rp, dtype, head_dim, s);
+  const hipError_t e = dtype == FSCHED_BF16 ? main_launch<Bf16>(a, p.main, head_dim, s)
+                                            : main_launch<F16>(a, p.main, head_dim, s);
   if (e != hipSuccess || !p.joins) return e;
   // requests with many rows: more blocks per request
   const int64_t most = (int64_t)a.max_q * a.group;

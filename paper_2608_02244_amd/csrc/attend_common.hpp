@@ -13,6 +13,7 @@
 
 namespace fs {
 
+constexpr int ATT_THREADS = 256, ATT_WAVES = ATT_THREADS / 64;
 constexpr float NEG_INF = -__builtin_inff();
 constexpr float LN2 = 0.6931471805599453f;
 

@@ -1,0 +1,8 @@
+// Attention kernels for f16 elements and heads of 64.
+#include "attend_main.hpp"
+
+namespace fs {
+
+template hipError_t launch_main<F16, 64>(const AttnArgs&, const MainPlan&, hipStream_t);
+
+}  // namespace fs

@@ -1,10 +1,21 @@
-// Attention for many rows (prompts, chunks, and every token's rows over a shared
-// prefix): launch descriptor of attend_tiles.hip.
+// Attention for many rows: prompts and chunks of them over what their request
+// holds, and the rows of all tokens over a shared prefix.
+//
+// A block takes 128 rows (tokens times the query heads of one key head, 32 per
+// wave) and goes over their keys in tiles, which its four waves share through
+// LDS; the next tile arrives by direct loads while one is worked on.
+//   S^T = K Q^T    32 keys x 32 rows, K rows from LDS, Q in registers
+//   O^T = V^T P^T  the scores leave the first product with a lane holding, of its
+//     row, keys 8g + 4h + 0..3 (h: half of the wave); the contraction takes them
+//     in that order, so P stays in its lanes, and the transposing LDS loads bring
+//     the values of those keys, one element of the head per lane.
+// A 16-byte piece c of key j lies at piece c ^ f(j) of its row, f a permutation of
+// the low bits that spreads both reads over all banks: the first takes one piece
+// of 32 keys at once, the second 64 bytes of 8 keys.
 #pragma once
 #include <hip/hip_runtime.h>
-#include <stdint.h>
 
-#include "step_common.hpp"
+#include "attend_common.hpp"
 
 namespace fs {
 
@@ -20,7 +31,349 @@ struct TilesPlan {
   float2* part_ml;   // [split][n_tok * q_heads] (mu, l)
 };
 
-hipError_t launch_attend_tiles(const AttnArgs& a, const TilesPlan& p, int dtype, int head_dim,
-                               hipStream_t s);
+template <int D>
+struct Tile {
+  static constexpr int KEYS = D == 256 ? 32 : 64;
+  static constexpr int PIECES = D / 8;                       // 16-byte pieces of a key
+  static constexpr int LOADS = KEYS * PIECES / ATT_THREADS;      // direct loads per thread
+  static constexpr int BYTES = KEYS * D * 2;
+  static __device__ __forceinline__ int swizzle(int key) {
+    return D == 64 ? (((key >> 1) & 1) << 2) | ((key >> 2) & 3)
+                   : ((key & 3) << 2) | ((key >> 2) & 3);
+  }
+};
+
+// 16 bytes per lane from global memory to LDS at base + 16 * lane.  The compiler
+// does not count these; they are waited for by hand before the block's barrier.
+__device__ __forceinline__ void load_to_lds(const void* src, uint32_t base) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, off"
+      :
+      : "v"(src), "s"(base)
+      : "memory", "m0");
+}
+
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+__device__ __forceinline__ u32x2 read_transposed(uint32_t addr) {
+  return __builtin_bit_cast(
+      u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)addr));
+}
+
+__device__ __forceinline__ u32x4 read16(uint32_t addr) {
+  return *(__attribute__((address_space(3))) u32x4*)(uintptr_t)addr;
+}
+
+template <class T, int D>
+__device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan& plan, int block,
+                                             char* lds) {
+  using L = Tile<D>;
+  constexpr int KB = L::KEYS, NT = KB / 32, QC = D / 16, DT = D / 32;
+  using elem = typename T::elem;
+  using x8 = typename T::x8;
+  // LDS: K and V of two tiles, then a few words
+  int(*reduce)[ATT_WAVES] = (int(*)[ATT_WAVES])(lds + 4 * L::BYTES);  // [2]
+  int* found_tile = reduce[2];                                        // [2]
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int col = lane & 31, h = lane >> 5;
+  const int shift = a.kv.page_shift, page_mask = (1 << shift) - 1;
+  int id = block;
+  const int kh = id % a.kv.kv_heads;
+  id /= a.kv.kv_heads;
+  const int part = id % plan.split;
+  int tile = id / plan.split;
+
+  // which rows: `tok` and `top` (index of the last key that it sees) of this lane's
+  Request x;
+  int r = 0, row0;  // row0: the block's first row among the request's (the step's) rows
+  int32_t* ints = (int32_t*)lds;
+  if (plan.prefix) {
+    row0 = tile * TILE_ROWS;
+    for (int i = tid; i <= a.n_req; i += ATT_THREADS) ints[i] = a.q_start[i];
+    __syncthreads();
+  } else {
+    // tiles of the requests before each: block-wide sums over all requests
+    const int n = a.n_req, per = (n + ATT_THREADS - 1) / ATT_THREADS;
+    const int r0 = min(n, tid * per), r1 = min(n, r0 + per);
+    auto tiles_of = [&](int i) {
+      const Request y = request_of(a, i);
+      const int rows = min(y.q_len, a.max_q) * a.group;
+      return rows > plan.min_rows ? (rows + TILE_ROWS - 1) / TILE_ROWS : 0;
+    };
+    int sum = 0;
+    for (int i = r0; i < r1; ++i) sum += tiles_of(i);
+    int s = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(s, d);
+      if (lane >= d) s += y;
+    }
+    if (lane == 63) reduce[0][wave] = s;
+    if (tid == 0) found_tile[0] = -1;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) s += reduce[0][w];
+    const int all = reduce[0][0] + reduce[0][1] + reduce[0][2] + reduce[0][3];
+    if (tile >= all) return;
+    tile = all - 1 - tile;  // the last rows of a prompt see most keys: they go first
+    int at = s - sum;
+    if (tile >= at && tile < s) {
+      for (int i = r0; i < r1; ++i) {
+        const int t = tiles_of(i);
+        if (tile < at + t) {
+          found_tile[0] = i;
+          found_tile[1] = tile - at;
+          break;
+        }
+        at += t;
+      }
+    }
+    __syncthreads();
+    r = found_tile[0];
+    row0 = found_tile[1] * TILE_ROWS;
+    x = request_of(a, r);
+  }
+
+  int tok = 0, top = -1, qh = kh * a.group;
+  bool on;
+  {
+    const int row = row0 + wave * 32 + col;
+    const int i = row / a.group;
+    const int g = row - i * a.group;
+    if (plan.prefix) {
+      on = i < a.n_tok;
+      if (on) {
+        int lo = 0, hi = a.n_req;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (ints[mid] <= i) lo = mid;
+          else hi = mid;
+        }
+        const Request y = request_of(a, lo);
+        on = i >= y.q0 && i - y.q0 < min(y.q_len, a.max_q);
+        top = on ? a.prefix_len + y.kv - y.q_len + (i - y.q0) : -1;
+        tok = i;
+      }
+    } else {
+      on = i < min(x.q_len, a.max_q);
+      top = on ? x.kv - x.q_len + i : -1;
+      tok = on ? x.q0 + i : x.q0;
+    }
+    if (on) qh += g;
+  }
+  const int n_held = plan.prefix ? a.prefix_len : x.kv;
+  const int offset = plan.prefix ? 0 : a.prefix_len;
+  const int sink_keys = a.window > 0 ? a.n_sink - offset : 0;
+  const int low = a.window > 0 ? top - a.window : -0x7fffffff - 1;
+  // first and last key index of the wave's rows, and of the block's
+  int wmin = on ? top : 0x7fffffff, wmax = on ? top : -0x7fffffff;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    wmin = min(wmin, __shfl_xor(wmin, d));
+    wmax = max(wmax, __shfl_xor(wmax, d));
+  }
+  __syncthreads();  // ints and reduce are read
+  if (lane == 0) {
+    reduce[0][wave] = wmin;
+    reduce[1][wave] = wmax;
+  }
+  __syncthreads();
+  const int bmin = min(min(reduce[0][0], reduce[0][1]), min(reduce[0][2], reduce[0][3]));
+  const int bmax = max(max(reduce[1][0], reduce[1][1]), max(reduce[1][2], reduce[1][3]));
+  wmin = uni_int(wmin);
+  wmax = uni_int(wmax);
+
+  // this part's tiles of keys
+  const int n_keys = max(0, min(n_held, bmax + 1));
+  Span sp = span_of<KB>(bmin, bmax, n_keys, a.window, a.n_sink, offset);
+  if (bmax < 0 || a.kv.n_pages == 0) sp.blocks = 0;
+  const int b0 = (int)((int64_t)sp.blocks * part / plan.split);
+  const int b1 = (int)((int64_t)sp.blocks * (part + 1) / plan.split);
+
+  x8 q[QC];
+  {
+    const elem* src =
+        (const elem*)a.q + (int64_t)tok * a.q_token + (int64_t)qh * a.q_head + h * 8;
+#pragma unroll
+    for (int c = 0; c < QC; ++c) q[c] = *(const x8*)(src + c * 16);
+  }
+  f32x16 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+  float mu = NEG_INF, l = 0.0f;
+
+  // LDS places: buffer b holds K at 2 b BYTES, V behind it
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const int f = L::swizzle(col);
+  uint32_t k_at[QC];  // key `col`, piece 2c + h
+#pragma unroll
+  for (int c = 0; c < QC; ++c)
+    k_at[c] = lds0 + col * (D * 2) + ((2 * c + h) ^ f) * 16;
+  uint32_t v_at[2][DT < 4 ? DT : 4];  // keys 4h + 8x + (lane mod 16) / 4, elements of tile dt
+#pragma unroll
+  for (int xx = 0; xx < 2; ++xx)
+#pragma unroll
+    for (int d = 0; d < (DT < 4 ? DT : 4); ++d) {
+      const int e = lane & 15, key = 4 * h + 8 * xx + (e >> 2);
+      const int piece = d * 4 + ((lane >> 4) & 1) * 2 + ((e & 3) >> 1);
+      v_at[xx][d] = lds0 + L::BYTES + key * (D * 2) + (piece ^ L::swizzle(key)) * 16 + (e & 1) * 8;
+    }
+
+  const int32_t* table = plan.prefix ? a.prefix_pages : a.table + (int64_t)r * a.width;
+  const elem* kbase = (const elem*)a.kv.k + kh * a.kv.k_head;
+  const elem* vbase = (const elem*)a.kv.v + kh * a.kv.v_head;
+  // page of key (lane mod KB) of tile b, -1 where no row of the block sees a key
+  auto page_at = [&](int b) {
+    const int s = sp.block(b) * KB + (lane & (KB - 1));
+    int p = -1;
+    if (b < b1 && s < n_keys && (a.window == 0 || s > bmin - a.window || s < sink_keys))
+      p = table[s >> shift];
+    return (uint32_t)p < (uint32_t)a.kv.n_pages ? p : -1;
+  };
+  // tile b to buffer `buf`; keys that are not there read page 0 (they are masked)
+  auto fetch = [&](int b, int page, int buf) {
+    const int s0 = sp.block(b) * KB;
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+      const int key = i * (ATT_THREADS / L::PIECES) + tid / L::PIECES;
+      const int piece = (tid % L::PIECES) ^ L::swizzle(key);
+      const int pg = max(0, __shfl(page, key));
+      const int slot = (s0 + key) & page_mask;
+      const uint32_t to = lds0 + buf * (2 * L::BYTES) + (i * ATT_THREADS + wave * 64) * 16;
+      load_to_lds(kbase + pg * a.kv.k_page + slot * a.kv.k_slot + piece * 8, uni_int(to));
+      load_to_lds(vbase + pg * a.kv.v_page + slot * a.kv.v_slot + piece * 8,
+                  uni_int(to + L::BYTES));
+    }
+  };
+
+  int page = page_at(b0), page_next = -1;
+  if (b0 < b1) {
+    fetch(b0, page, 0);
+    page_next = page_at(b0 + 1);
+  }
+  for (int b = b0; b < b1; ++b) {
+    const int buf = (b - b0) & 1;
+    wait_loads();
+    __syncthreads();  // tile b is there; the other buffer is free
+    const uint64_t found = __ballot(page >= 0);
+    if (b + 1 < b1) fetch(b + 1, page_next, buf ^ 1);
+    page = page_next;
+    page_next = page_at(b + 2);
+
+    const int s0 = sp.block(b) * KB;
+    if (s0 > wmax || (a.window > 0 && s0 + KB - 1 <= wmin - a.window && s0 >= sink_keys)) continue;
+    const bool full = found == ~0ull && s0 + KB - 1 <= wmin &&
+                      (a.window == 0 || s0 > wmax - a.window || s0 + KB <= sink_keys);
+    const uint32_t shift_b = buf * (2 * L::BYTES);
+
+    f32x16 s[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < QC; ++c)
+        s[t] = T::mfma32(__builtin_bit_cast(x8, read16(k_at[c] + shift_b + t * 32 * D * 2)), q[c],
+                         s[t]);
+    }
+    if (!full) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = t * 32 + 8 * (i / 4) + 4 * h + (i % 4), key = s0 + j;
+          const bool see = ((found >> j) & 1) && key <= top && (key > low || key < sink_keys);
+          if (!see) s[t][i] = NEG_INF;
+        }
+    }
+    float mx = NEG_INF;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
+    mx = max_xor32(mx) * a.scale_log2 - BIAS<T>;
+    if (__ballot(mx > mu + TAU)) {
+      const float to = mx > mu + TAU ? mx : mu;
+      const float g = part_scale(mu, to);
+      mu = to;
+      l *= g;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= g;
+    }
+    const float base = mu == NEG_INF ? 0.0f : mu;
+    x8 p[2 * NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = exp2_fast(fmaf(s[t][i], a.scale_log2, -base));
+        l += e;
+        p[2 * t + i / 8][i % 8] = (elem)e;  // rounded to the type of the values
+      }
+    const bool holes = found != ~0ull;
+#pragma unroll
+    for (int g = 0; g < 2 * NT; ++g) {
+      u32x4 keep = {~0u, ~0u, ~0u, ~0u};  // values of keys that are not there become 0
+      if (holes) {
+        const uint32_t bits = (uint32_t)(found >> (16 * g + 4 * h));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = (i >> 1) * 8 + (i & 1) * 2;
+          keep[i] = ((bits >> j) & 1 ? 0xffffu : 0u) | ((bits >> (j + 1)) & 1 ? 0xffff0000u : 0u);
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const uint32_t more = shift_b + g * 16 * D * 2 + (d / 4) * 256;
+        const u32x2 lo = read_transposed(v_at[0][d % 4] + more);
+        const u32x2 hi = read_transposed(v_at[1][d % 4] + more);
+        u32x4 y = {lo[0], lo[1], hi[0], hi[1]};
+        if (holes) y &= keep;
+        o[d] = T::mfma32(__builtin_bit_cast(x8, y), p[g], o[d]);
+      }
+    }
+  }
+
+  l = sum_xor32(l);
+  if (plan.parts) {
+    if (!on) return;
+    const int64_t at = ((int64_t)part * a.n_tok + tok) * a.q_heads + qh;
+    if (h == 0) plan.part_ml[at] = make_float2(mu, l);
+    float* dst = plan.part_o + at * D + 4 * h;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(dst + d * 32 + i * 8) =
+            (f32x4){o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+    return;
+  }
+  if (!on) return;
+  const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+  elem* dst = (elem*)a.out + (int64_t)tok * a.o_token + (int64_t)qh * a.o_head + 4 * h;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x2 y = {pack2<T>(o[d][4 * i] * inv, o[d][4 * i + 1] * inv),
+                       pack2<T>(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv)};
+      *(u32x2*)(dst + d * 32 + i * 8) = y;
+    }
+  if (a.lse && h == 0) a.lse[(int64_t)tok * a.q_heads + qh] = (mu + log2f(l)) * LN2;
+}
+
+template <int D>
+constexpr size_t tiles_lds() {
+  return 4 * (size_t)Tile<D>::BYTES + 256;
+}
 
 }  // namespace fs

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(THREADS) void qk_rope_kernel(RopeArgs a, int chunks
   for (int h = h0 + grp; h - grp < h1; h += HEADS) {
     const bool on = h < h1;  // lanes past the last head help their wave's exchanges
     x8 raw = {};
-    if (on) raw = *(const x8*)(in + (int64_t)h * D);
+    if (on) raw = __builtin_nontemporal_load((const x8*)(in + (int64_t)h * D));
     const bool is_q = h < a.q_heads, is_k = !is_q && h < a.q_heads + a.kv.kv_heads;
     float x[8];
     float sq = 0.0f;

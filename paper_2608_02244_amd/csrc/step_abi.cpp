@@ -23,6 +23,7 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool stride_ok(int64_t s) { return s >= 0 && (s & 7) == 0; }
 
 constexpr int32_t kMaxPage = 65536, kMaxHeads = 1024;
+constexpr int64_t kMaxStride = (int64_t)1 << 40, kMaxInPage = (int64_t)1 << 27;
 
 int check_flags(uint32_t flags) {
   if (!(flags & FSCHED_F_DEVICE_PTRS)) return FSCHED_EINVAL;
@@ -42,6 +43,11 @@ int check_cache(const fsched_kv_cache* c) {
   if (!aligned16(c->k) || !aligned16(c->v)) return FSCHED_EINVAL;
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return FSCHED_ENOTIMPL;
   if (c->page_size > kMaxPage || c->kv_heads > kMaxHeads) return FSCHED_ETOOLARGE;
+  // kernels take byte offsets within a page in 32 bits
+  for (int i = 0; i < 3; ++i)
+    if (c->k_stride[i] > kMaxStride || c->v_stride[i] > kMaxStride) return FSCHED_ETOOLARGE;
+  if (c->k_stride[2] * c->page_size > kMaxInPage || c->v_stride[2] * c->page_size > kMaxInPage)
+    return FSCHED_ETOOLARGE;
   return FSCHED_OK;
 }
 
