@@ -14,6 +14,7 @@
 namespace fs {
 
 constexpr int ATT_THREADS = 256, ATT_WAVES = ATT_THREADS / 64;
+constexpr int WIDE_SHIFT = 4;  // the kernels' WIDE forms are for pages of 2^4 tokens and more
 constexpr float NEG_INF = -__builtin_inff();
 constexpr float LN2 = 0.6931471805599453f;
 

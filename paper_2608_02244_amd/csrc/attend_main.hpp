@@ -24,13 +24,13 @@ __global__ __launch_bounds__(ATT_THREADS, rows_occupancy(D, RT, WIDE)) void atte
   attend_rows<T, D, RT, WIDE>(a, p.rows, blockIdx.x, lds);
 }
 
-template <class T, int D>
+template <class T, int D, bool WIDE>
 __global__ __launch_bounds__(ATT_THREADS, D == 256 ? 1 : 2) void attend_tiles_kernel(AttnArgs a,
                                                                                      MainPlan p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int b = blockIdx.x;
   const bool pre = b < p.pre_blocks;
-  attend_tiles<T, D>(a, pre ? p.pre : p.own, pre ? b : b - p.pre_blocks, lds);
+  attend_tiles<T, D, WIDE>(a, pre ? p.pre : p.own, pre ? b : b - p.pre_blocks, lds);
 }
 
 template <class T, int D, int RT, bool WIDE>
@@ -44,7 +44,19 @@ __global__ __launch_bounds__(ATT_THREADS, D == 256 ? 1 : 2) void attend_both_ker
   }
   b -= p.rows_blocks;
   const bool pre = b < p.pre_blocks;
-  attend_tiles<T, D>(a, pre ? p.pre : p.own, pre ? b : b - p.pre_blocks, lds);
+  attend_tiles<T, D, WIDE>(a, pre ? p.pre : p.own, pre ? b : b - p.pre_blocks, lds);
+}
+
+inline hipError_t launch_with_lds(void (*kernel)(AttnArgs, MainPlan), dim3 grid, dim3 block,
+                                  size_t lds, const AttnArgs& a, const MainPlan& p,
+                                  hipStream_t s) {
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(
+        (const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<grid, block, lds, s>>>(a, p);
+  return hipGetLastError();
 }
 
 template <class T, int D, int RT>
@@ -55,13 +67,7 @@ hipError_t launch_main_rows(const AttnArgs& a, const MainPlan& p, hipStream_t s)
   void (*kernel)(AttnArgs, MainPlan) =
       tiles ? (wide ? attend_both_kernel<T, D, RT, true> : attend_both_kernel<T, D, RT, false>)
             : (wide ? attend_rows_kernel<T, D, RT, true> : attend_rows_kernel<T, D, RT, false>);
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(
-        (const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  kernel<<<grid, block, lds, s>>>(a, p);
-  return hipGetLastError();
+  return launch_with_lds(kernel, grid, block, lds, a, p, s);
 }
 
 // One translation unit per element type and head size instantiates this.
@@ -72,15 +78,12 @@ hipError_t launch_main(const AttnArgs& a, const MainPlan& p, hipStream_t s) {
       if (p.rows.row_tiles == 2) return launch_main_rows<T, D, 2>(a, p, s);
     return launch_main_rows<T, D, 1>(a, p, s);
   }
+  const dim3 grid((unsigned)(p.pre_blocks + p.own_blocks)), block(ATT_THREADS);
   const size_t lds = tiles_lds<D>();
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)attend_tiles_kernel<T, D>,
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  attend_tiles_kernel<T, D><<<dim3((unsigned)(p.pre_blocks + p.own_blocks)), dim3(ATT_THREADS),
-                              lds, s>>>(a, p);
-  return hipGetLastError();
+  void (*kernel)(AttnArgs, MainPlan) = a.kv.page_shift >= WIDE_SHIFT
+                                           ? attend_tiles_kernel<T, D, true>
+                                           : attend_tiles_kernel<T, D, false>;
+  return launch_with_lds(kernel, grid, block, lds, a, p, s);
 }
 
 extern template hipError_t launch_main<Bf16, 64>(const AttnArgs&, const MainPlan&, hipStream_t);

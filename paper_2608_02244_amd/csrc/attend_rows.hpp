@@ -44,7 +44,6 @@ struct RowsPlan {
 };
 
 constexpr int UNIT = 32;       // keys of a unit
-constexpr int WIDE_SHIFT = 4;  // pages of 2^4 tokens and more
 constexpr int MIN_PIECE = 2;   // units of a wave, at least
 
 // Blocks per compute unit that the registers allow.

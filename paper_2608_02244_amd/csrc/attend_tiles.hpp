@@ -55,6 +55,17 @@ __device__ __forceinline__ void load_to_lds(const void* src, uint32_t base) {
       : "memory", "m0");
 }
 
+// The same from base + off, the base uniform.
+__device__ __forceinline__ void load_to_lds(const char* src, uint32_t off, uint32_t base) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, %1"
+      :
+      : "v"(off), "s"(src), "s"(base)
+      : "memory", "m0");
+}
+
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -69,7 +80,14 @@ __device__ __forceinline__ u32x4 read16(uint32_t addr) {
   return *(__attribute__((address_space(3))) u32x4*)(uintptr_t)addr;
 }
 
-template <class T, int D>
+__device__ __forceinline__ void write16(uint32_t addr, u32x4 v) {
+  *(__attribute__((address_space(3))) u32x4*)(uintptr_t)addr = v;
+}
+
+// WIDE: pages of 16 tokens and more.  The keys that a wave loads at once (8, 4 or 2,
+// from a multiple of that on) then lie in one page, and their addresses are uniform but
+// for a lane's constant offset.
+template <class T, int D, bool WIDE>
 __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan& plan, int block,
                                              char* lds) {
   using L = Tile<D>;
@@ -227,62 +245,116 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
     }
 
   const int32_t* table = plan.prefix ? a.prefix_pages : a.table + (int64_t)r * a.width;
-  const elem* kbase = (const elem*)a.kv.k + kh * a.kv.k_head;
-  const elem* vbase = (const elem*)a.kv.v + kh * a.kv.v_head;
-  // page of key (lane mod KB) of tile b, -1 where no row of the block sees a key
-  auto page_at = [&](int b) {
-    const int s = sp.block(b) * KB + (lane & (KB - 1));
-    int p = -1;
-    if (b < b1 && s < n_keys && (a.window == 0 || s > bmin - a.window || s < sink_keys))
-      p = table[s >> shift];
-    return (uint32_t)p < (uint32_t)a.kv.n_pages ? p : -1;
+  const char* kbase = (const char*)((const elem*)a.kv.k + kh * a.kv.k_head);
+  const char* vbase = (const char*)((const elem*)a.kv.v + kh * a.kv.v_head);
+  const uint32_t k_slot = (uint32_t)a.kv.k_slot * 2, v_slot = (uint32_t)a.kv.v_slot * 2;
+  // Key (lane mod KB) of tile b: whether some row of the block sees it, and its page (for
+  // keys past the last one the last one's); looked at only when its turn comes.
+  auto key_at = [&](int b) { return sp.block(b) * KB + (lane & (KB - 1)); };
+  auto seen = [&](int s) {
+    return s < n_keys && (a.window == 0 || s > bmin - a.window || s < sink_keys);
   };
+  auto page_at = [&](int b) { return table[min(key_at(b), n_keys - 1) >> shift]; };
+  auto in_cache = [&](int page) { return (uint32_t)page < (uint32_t)a.kv.n_pages; };
   // tile b to buffer `buf`; keys that are not there read page 0 (they are masked)
   auto fetch = [&](int b, int page, int buf) {
     const int s0 = sp.block(b) * KB;
+    constexpr int AT_ONCE = ATT_THREADS / L::PIECES, PER_WAVE = 64 / L::PIECES;
 #pragma unroll
     for (int i = 0; i < L::LOADS; ++i) {
-      const int key = i * (ATT_THREADS / L::PIECES) + tid / L::PIECES;
-      const int piece = (tid % L::PIECES) ^ L::swizzle(key);
-      const int pg = max(0, __shfl(page, key));
-      const int slot = (s0 + key) & page_mask;
-      const uint32_t to = lds0 + buf * (2 * L::BYTES) + (i * ATT_THREADS + wave * 64) * 16;
-      load_to_lds(kbase + pg * a.kv.k_page + slot * a.kv.k_slot + piece * 8, uni_int(to));
-      load_to_lds(vbase + pg * a.kv.v_page + slot * a.kv.v_slot + piece * 8,
-                  uni_int(to + L::BYTES));
+      const uint32_t to = uni_int(lds0 + buf * (2 * L::BYTES) + (i * ATT_THREADS + wave * 64) * 16);
+      const int key = i * AT_ONCE + tid / L::PIECES;
+      const uint32_t piece = ((tid % L::PIECES) ^ L::swizzle(key)) * 16;
+      if constexpr (WIDE) {
+        const int first = uni_int(i * AT_ONCE + wave * PER_WAVE);
+        const int there = __builtin_amdgcn_readlane(page, first);
+        const uint32_t pg = in_cache(there) ? there : 0;
+        const uint32_t slot = (s0 + first) & page_mask, mine = lane / L::PIECES;
+        load_to_lds(kbase + pg * (uint64_t)(a.kv.k_page * 2) + slot * (uint64_t)k_slot,
+                    mine * k_slot + piece, to);
+        load_to_lds(vbase + pg * (uint64_t)(a.kv.v_page * 2) + slot * (uint64_t)v_slot,
+                    mine * v_slot + piece, to + L::BYTES);
+      } else {
+        const int there = __shfl(page, key);
+        const uint32_t pg = in_cache(there) ? there : 0;
+        const uint32_t slot = (s0 + key) & page_mask;
+        load_to_lds(kbase + pg * (uint64_t)(a.kv.k_page * 2) + slot * k_slot + piece, to);
+        load_to_lds(vbase + pg * (uint64_t)(a.kv.v_page * 2) + slot * v_slot + piece,
+                    to + L::BYTES);
+      }
     }
   };
 
-  int page = page_at(b0), page_next = -1;
+  int page = 0, page_next = 0;
   if (b0 < b1) {
+    page = page_at(b0);
     fetch(b0, page, 0);
-    page_next = page_at(b0 + 1);
+    if (b0 + 1 < b1) page_next = page_at(b0 + 1);
   }
   for (int b = b0; b < b1; ++b) {
     const int buf = (b - b0) & 1;
     wait_loads();
     __syncthreads();  // tile b is there; the other buffer is free
-    const uint64_t found = __ballot(page >= 0);
+    const uint64_t found = __ballot(seen(key_at(b)) && in_cache(page));
     if (b + 1 < b1) fetch(b + 1, page_next, buf ^ 1);
     page = page_next;
-    page_next = page_at(b + 2);
+    if (b + 2 < b1) page_next = page_at(b + 2);
 
     const int s0 = sp.block(b) * KB;
+    const uint32_t shift_b = buf * (2 * L::BYTES);
+    if (found != ~0ull) {
+      // keys that are not there (the same ones for all waves): their values become 0, since
+      // 0 * NaN would be NaN
+#pragma unroll
+      for (int i = 0; i < L::LOADS; ++i) {
+        const int key = i * (ATT_THREADS / L::PIECES) + tid / L::PIECES;
+        if (!((found >> key) & 1))
+          write16(lds0 + shift_b + L::BYTES + (i * ATT_THREADS + tid) * 16, (u32x4){0, 0, 0, 0});
+      }
+      __syncthreads();
+    }
     if (s0 > wmax || (a.window > 0 && s0 + KB - 1 <= wmin - a.window && s0 >= sink_keys)) continue;
     const bool full = found == ~0ull && s0 + KB - 1 <= wmin &&
                       (a.window == 0 || s0 > wmax - a.window || s0 + KB <= sink_keys);
-    const uint32_t shift_b = buf * (2 * L::BYTES);
 
     f32x16 s[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+    uint32_t k_of[QC];
 #pragma unroll
-      for (int c = 0; c < QC; ++c)
-        s[t] = T::mfma32(__builtin_bit_cast(x8, read16(k_at[c] + shift_b + t * 32 * D * 2)), q[c],
-                         s[t]);
+    for (int c = 0; c < QC; ++c) k_of[c] = k_at[c] + shift_b;
+    u32x4 kf[2][NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) kf[0][t] = read16(k_of[0] + t * 32 * D * 2);
+#pragma unroll
+    for (int c = 0; c < QC; ++c) {
+      if (c + 1 < QC) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) kf[(c + 1) & 1][t] = read16(k_of[c + 1] + t * 32 * D * 2);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        s[t] = T::mfma32(__builtin_bit_cast(x8, kf[c & 1][t]), q[c], s[t]);
     }
+    // the values' first operands arrive while the weights are computed
+    uint32_t v_of[2][DT < 4 ? DT : 4];
+#pragma unroll
+    for (int xx = 0; xx < 2; ++xx)
+#pragma unroll
+      for (int d = 0; d < (DT < 4 ? DT : 4); ++d) v_of[xx][d] = v_at[xx][d] + shift_b;
+    auto values = [&](int g, int d) {
+      const int more = g * 16 * D * 2 + (d / 4) * 256;
+      const u32x2 lo = read_transposed(v_of[0][d % 4] + more);
+      const u32x2 hi = read_transposed(v_of[1][d % 4] + more);
+      return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+    };
+    u32x4 vf[2][DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) vf[0][d] = values(0, d);
+    __builtin_amdgcn_sched_barrier(0);
     if (!full) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -310,36 +382,29 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
         for (int i = 0; i < 16; ++i) o[d][i] *= g;
     }
     const float base = mu == NEG_INF ? 0.0f : mu;
-    x8 p[2 * NT];
+    // 16 keys at a time: the weights of the next are computed, and their values read,
+    // beside the products of these
+    x8 p[2];
+    auto weights = [&](int g) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = exp2_fast(fmaf(s[t][i], a.scale_log2, -base));
+      for (int i = 0; i < 8; ++i) {
+        const float e = exp2_fast(fmaf(s[g / 2][8 * (g & 1) + i], a.scale_log2, -base));
         l += e;
-        p[2 * t + i / 8][i % 8] = (elem)e;  // rounded to the type of the values
+        p[g & 1][i] = (elem)e;  // rounded to the type of the values, as the products need
       }
-    const bool holes = found != ~0ull;
+    };
+    weights(0);
 #pragma unroll
     for (int g = 0; g < 2 * NT; ++g) {
-      u32x4 keep = {~0u, ~0u, ~0u, ~0u};  // values of keys that are not there become 0
-      if (holes) {
-        const uint32_t bits = (uint32_t)(found >> (16 * g + 4 * h));
+      if (g + 1 < 2 * NT) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int j = (i >> 1) * 8 + (i & 1) * 2;
-          keep[i] = ((bits >> j) & 1 ? 0xffffu : 0u) | ((bits >> (j + 1)) & 1 ? 0xffff0000u : 0u);
-        }
+        for (int d = 0; d < DT; ++d) vf[(g + 1) & 1][d] = values(g + 1, d);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      if (g + 1 < 2 * NT) weights(g + 1);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const uint32_t more = shift_b + g * 16 * D * 2 + (d / 4) * 256;
-        const u32x2 lo = read_transposed(v_at[0][d % 4] + more);
-        const u32x2 hi = read_transposed(v_at[1][d % 4] + more);
-        u32x4 y = {lo[0], lo[1], hi[0], hi[1]};
-        if (holes) y &= keep;
-        o[d] = T::mfma32(__builtin_bit_cast(x8, y), p[g], o[d]);
-      }
+      for (int d = 0; d < DT; ++d)
+        o[d] = T::mfma32(__builtin_bit_cast(x8, vf[g & 1][d]), p[g & 1], o[d]);
     }
   }
 
