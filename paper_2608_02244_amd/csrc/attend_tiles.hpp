@@ -84,6 +84,17 @@ __device__ __forceinline__ void write16(uint32_t addr, u32x4 v) {
   *(__attribute__((address_space(3))) u32x4*)(uintptr_t)addr = v;
 }
 
+__device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane);
+  return (uint64_t)hi << 32 | lo;
+}
+
+__device__ __forceinline__ uint64_t shuffled(uint64_t x, int lane) {
+  const uint32_t lo = __shfl((int)(uint32_t)x, lane), hi = __shfl((int)(uint32_t)(x >> 32), lane);
+  return (uint64_t)hi << 32 | lo;
+}
+
 // WIDE: pages of 16 tokens and more.  The keys that a wave loads at once (8, 4 or 2,
 // from a multiple of that on) then lie in one page, and their addresses are uniform but
 // for a lane's constant offset.
@@ -256,10 +267,13 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
   };
   auto page_at = [&](int b) { return table[min(key_at(b), n_keys - 1) >> shift]; };
   auto in_cache = [&](int page) { return (uint32_t)page < (uint32_t)a.kv.n_pages; };
-  // tile b to buffer `buf`; keys that are not there read page 0 (they are masked)
+  // tile b to buffer `buf`; keys that are not in the cache read page 0 (they are masked).
+  // A lane computes the addresses of key (lane mod KB), and the loads take them from there.
   auto fetch = [&](int b, int page, int buf) {
-    const int s0 = sp.block(b) * KB;
     constexpr int AT_ONCE = ATT_THREADS / L::PIECES, PER_WAVE = 64 / L::PIECES;
+    const uint32_t pg = in_cache(page) ? page : 0, slot = key_at(b) & page_mask;
+    const uint64_t k_from = (uint64_t)kbase + pg * (uint64_t)(a.kv.k_page * 2) + slot * k_slot;
+    const uint64_t v_from = (uint64_t)vbase + pg * (uint64_t)(a.kv.v_page * 2) + slot * v_slot;
 #pragma unroll
     for (int i = 0; i < L::LOADS; ++i) {
       const uint32_t to = uni_int(lds0 + buf * (2 * L::BYTES) + (i * ATT_THREADS + wave * 64) * 16);
@@ -267,20 +281,12 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
       const uint32_t piece = ((tid % L::PIECES) ^ L::swizzle(key)) * 16;
       if constexpr (WIDE) {
         const int first = uni_int(i * AT_ONCE + wave * PER_WAVE);
-        const int there = __builtin_amdgcn_readlane(page, first);
-        const uint32_t pg = in_cache(there) ? there : 0;
-        const uint32_t slot = (s0 + first) & page_mask, mine = lane / L::PIECES;
-        load_to_lds(kbase + pg * (uint64_t)(a.kv.k_page * 2) + slot * (uint64_t)k_slot,
-                    mine * k_slot + piece, to);
-        load_to_lds(vbase + pg * (uint64_t)(a.kv.v_page * 2) + slot * (uint64_t)v_slot,
-                    mine * v_slot + piece, to + L::BYTES);
+        const uint32_t mine = lane / L::PIECES;
+        load_to_lds((const char*)lane_of(k_from, first), mine * k_slot + piece, to);
+        load_to_lds((const char*)lane_of(v_from, first), mine * v_slot + piece, to + L::BYTES);
       } else {
-        const int there = __shfl(page, key);
-        const uint32_t pg = in_cache(there) ? there : 0;
-        const uint32_t slot = (s0 + key) & page_mask;
-        load_to_lds(kbase + pg * (uint64_t)(a.kv.k_page * 2) + slot * k_slot + piece, to);
-        load_to_lds(vbase + pg * (uint64_t)(a.kv.v_page * 2) + slot * v_slot + piece,
-                    to + L::BYTES);
+        load_to_lds((const char*)shuffled(k_from, key) + piece, to);
+        load_to_lds((const char*)shuffled(v_from, key) + piece, to + L::BYTES);
       }
     }
   };
@@ -356,13 +362,15 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
     for (int d = 0; d < DT; ++d) vf[0][d] = values(0, d);
     __builtin_amdgcn_sched_barrier(0);
     if (!full) {
+      const uint64_t mine = found >> (4 * h);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int j = t * 32 + 8 * (i / 4) + 4 * h + (i % 4), key = s0 + j;
-          const bool see = ((found >> j) & 1) && key <= top && (key > low || key < sink_keys);
-          if (!see) s[t][i] = NEG_INF;
+          const int at = t * 32 + 8 * (i / 4) + (i % 4), key = s0 + at + 4 * h;
+          const bool see = (bool)((mine >> at) & 1) & (key <= top) &
+                           ((key > low) | (key < sink_keys));
+          s[t][i] = see ? s[t][i] : NEG_INF;
         }
     }
     float mx = NEG_INF;
