@@ -33,11 +33,9 @@ struct JoinArgs {
 // Running join of parts of one row, 8 elements of it.
 struct Joined {
   float m = NEG_INF, l = 0.0f, o[8] = {};
-  __device__ __forceinline__ void add(float2 ml, const float* src) {
-    if (ml.x == NEG_INF) return;
+  __device__ __forceinline__ void add(float2 ml, f32x4 y, f32x4 z) {
     const float to = fmaxf(m, ml.x);
-    const float f = part_scale(m, to), g = exp2_fast(ml.x - to);
-    const f32x4 y = *(const f32x4*)src, z = *(const f32x4*)(src + 4);
+    const float f = part_scale(m, to), g = part_scale(ml.x, to);
     m = to;
     l = l * f + ml.y * g;
 #pragma unroll
@@ -48,50 +46,69 @@ struct Joined {
   }
 };
 
-// One block per request, key head and group of ROWS rows; D/8 threads hold a row,
-// and where there are fewer rows than that fills, several such groups share its parts.
+// Blocks for each request; D/8 threads hold a row (of any key head), and where there
+// are fewer rows than that fills, several such groups share a row's parts.  Bound by
+// latency (few parts) or by the parts' bytes: four parts of a row are read at once.
 template <class T, int D>
 __global__ __launch_bounds__(THREADS) void attend_join_kernel(AttnArgs a, JoinArgs j) {
-  constexpr int LANES = D / 8, GROUPS = THREADS / LANES;
+  constexpr int LANES = D / 8, GROUPS = THREADS / LANES, AHEAD = 4;
   using elem = typename T::elem;
   using x8 = typename T::x8;
   __shared__ float other[GROUPS][D + 4];
   __shared__ float2 other_ml[GROUPS];
-  const int r = blockIdx.x % a.n_req, kh = blockIdx.x / a.n_req;
+  const int r = blockIdx.x;
   const Request x = request_of(a, r);
-  const int rows = min(x.q_len, a.max_q) * a.group;
-  if (rows == 0) return;
-  const bool few = rows <= j.row_limit;
-  RowsTile t = {0, 0, 0, 0};
-  if (few) t = j.tiles[(int64_t)kh * a.n_req + r];
-  const int own = few ? t.count : j.own_split;
-  if (j.pre_split == 0 && (few ? own <= 1 : own == 0)) return;  // written already
+  const int head_rows = min(x.q_len, a.max_q) * a.group;  // of one key head
+  const bool few = head_rows <= j.row_limit;
+  if (head_rows == 0 || (!few && j.own_split + j.pre_split == 0)) return;  // nothing, or written
 
   const int grp = threadIdx.x / LANES, d0 = (threadIdx.x % LANES) * 8;
+  const int rows = head_rows * a.kv.kv_heads;
+  const int per = (rows + gridDim.y - 1) / gridDim.y;  // rows of a block
+  const int end = min(rows, per * ((int)blockIdx.y + 1));
   int at_once = 1;  // rows at once; GROUPS / at_once groups share one
-  while (at_once < rows && at_once < GROUPS) at_once *= 2;
+  while (at_once < per && at_once < GROUPS) at_once *= 2;
   const int share = GROUPS / at_once, mine = grp / at_once, sub = grp % at_once;
-  const int parts = own + j.pre_split;
-  for (int base = blockIdx.y * at_once; base < rows; base += gridDim.y * at_once) {
-    const int row = base + sub;
-    const bool on = row < rows;
-    const int tok = x.q0 + (on ? row / a.group : 0);
-    const int qh = kh * a.group + (on ? row % a.group : 0);
-    const int64_t th = (int64_t)tok * a.q_heads + qh, all = (int64_t)a.n_tok * a.q_heads;
+  const int64_t all = (int64_t)a.n_tok * a.q_heads;
+  for (int base = blockIdx.y * per; base < end; base += at_once) {
+    const bool on = base + sub < end;
+    const int kh = on ? (base + sub) / head_rows : 0;
+    const int row = on ? base + sub - kh * head_rows : 0;
+    const int tok = x.q0 + row / a.group, qh = kh * a.group + row % a.group;
+    const int64_t th = (int64_t)tok * a.q_heads + qh;
+    RowsTile t = {0, 0, 0, 0};
+    if (few) t = j.tiles[(int64_t)kh * a.n_req + r];
+    const int own = few ? t.count : j.own_split;
+    // a single part was written as the result
+    const int parts = j.pre_split == 0 && few && own <= 1 ? 0 : own + j.pre_split;
     Joined s;
     if (on) {
-      for (int i = mine; i < parts; i += share) {
-        if (i >= own) {
-          const int64_t at = (int64_t)(i - own) * all + th;
-          s.add(j.pre_ml[at], j.pre_o + at * D + d0);
-        } else if (few) {
-          const int64_t slot = i == 0 ? t.first : 2 * ((int64_t)t.wave + i);
-          const int64_t at = slot * j.slot_rows + row;
-          s.add(j.rows_ml[at], j.rows_o + at * D + d0);
-        } else {
-          const int64_t at = (int64_t)i * all + th;
-          s.add(j.own_ml[at], j.own_o + at * D + d0);
+      for (int i0 = mine; i0 < parts; i0 += AHEAD * share) {
+        float2 ml[AHEAD];
+        f32x4 y[AHEAD], z[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          const bool more = i0 + k * share < parts;
+          const int i = more ? i0 + k * share : i0;
+          const float2* from;
+          const float* o;
+          if (i >= own) {
+            const int64_t at = (int64_t)(i - own) * all + th;
+            from = j.pre_ml + at;
+            o = j.pre_o + at * D;
+          } else {
+            const int64_t slot = i == 0 ? t.first : 2 * ((int64_t)t.wave + i);
+            const int64_t at = few ? slot * j.slot_rows + row : (int64_t)i * all + th;
+            from = (few ? j.rows_ml : j.own_ml) + at;
+            o = (few ? j.rows_o : j.own_o) + at * D;
+          }
+          ml[k] = *from;
+          y[k] = *(const f32x4*)(o + d0);
+          z[k] = *(const f32x4*)(o + d0 + 4);
+          if (!more) ml[k] = make_float2(NEG_INF, 0.0f);
         }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) s.add(ml[k], y[k], z[k]);
       }
     }
     if (share > 1) {
@@ -102,10 +119,12 @@ __global__ __launch_bounds__(THREADS) void attend_join_kernel(AttnArgs a, JoinAr
       if (d0 == 0) other_ml[grp] = make_float2(s.m, s.l);
       __syncthreads();
       if (mine == 0)
-        for (int i = 1; i < share; ++i)
-          s.add(other_ml[i * at_once + sub], &other[i * at_once + sub][d0]);
+        for (int i = 1; i < min(share, parts); ++i) {
+          const float* o = &other[i * at_once + sub][d0];
+          s.add(other_ml[i * at_once + sub], *(const f32x4*)o, *(const f32x4*)(o + 4));
+        }
     }
-    if (mine == 0 && on) {
+    if (mine == 0 && on && parts > 0) {
       const float inv = s.l > 0.0f ? 1.0f / s.l : s.l == 0.0f ? 0.0f : s.l;
       x8 out;
 #pragma unroll
@@ -166,10 +185,11 @@ Shape plan(const AttnArgs& a, int head_dim, int n_cu, char* ws) {
     p.join.rows_ml = rp.part_ml;
     p.join.tiles = rp.tiles;
   }
-  // Keys are cut so that about two blocks per compute unit have work, none with
-  // fewer than 256 keys.
+  // Keys are cut so that the places beside the rows blocks have work, none fewer than
+  // 256 keys: parts cost their bytes twice.
+  const int64_t places = (with_rows ? 1 : 2) * (int64_t)n_cu;
   auto cut = [&](int64_t tiles, int64_t keys) {
-    const int64_t want = (2 * (int64_t)n_cu + tiles * a.kv.kv_heads - 1) / (tiles * a.kv.kv_heads);
+    const int64_t want = (places + tiles * a.kv.kv_heads - 1) / (tiles * a.kv.kv_heads);
     const int64_t can = keys / 256 > 1 ? keys / 256 : 1;
     const int64_t s = want < can ? want : can;
     return (int)(s < 1 ? 1 : s);
@@ -239,10 +259,15 @@ hipError_t launch_attend(const AttnArgs& a, int dtype, int head_dim, int n_cu, v
   const hipError_t e = dtype == FSCHED_BF16 ? main_launch<Bf16>(a, p.main, head_dim, s)
                                             : main_launch<F16>(a, p.main, head_dim, s);
   if (e != hipSuccess || !p.joins) return e;
-  // requests with many rows: more blocks per request
-  const int64_t most = (int64_t)a.max_q * a.group;
-  const unsigned y = (unsigned)(most <= 64 ? 1 : most / 64 < 256 ? most / 64 : 256);
-  const dim3 grid((unsigned)(a.n_req * a.kv.kv_heads), y);
+  // enough blocks to fill the device, of at most 64 rows and at least one
+  const int64_t most = p.join.own_split + p.join.pre_split > 0 ? (int64_t)a.max_q * a.q_heads
+                                                               : p.join.slot_rows * a.kv.kv_heads;
+  int64_t y = (8 * n_cu + a.n_req - 1) / a.n_req;
+  if (y < most / 64) y = most / 64;
+  if (y > most) y = most;
+  if (y > 1024) y = 1024;
+  if (y < 1) y = 1;
+  const dim3 grid((unsigned)a.n_req, (unsigned)y);
   if (dtype == FSCHED_BF16) join<Bf16>(a, p.join, head_dim, grid, s);
   else join<F16>(a, p.join, head_dim, grid, s);
   return hipGetLastError();

@@ -44,7 +44,7 @@ struct RowsPlan {
 };
 
 constexpr int UNIT = 32;       // keys of a unit
-constexpr int MIN_PIECE = 2;   // units of a wave, at least
+constexpr int MOST_PARTS = 32;  // of a tile, on average
 
 // Blocks per compute unit that the registers allow.
 constexpr int rows_occupancy(int D, int RT, bool wide) {
@@ -111,8 +111,10 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const RowsPlan& p
   auto quotient = [](int64_t x, int64_t y) {  // a 64-bit division is some 130 instructions
     return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
   };
-  const int64_t piece =
-      max((int64_t)MIN_PIECE, quotient(total + plan.waves - 1, plan.waves));
+  // a few tiles are not cut finer than their parts are worth reading again
+  const int64_t at_most = (int64_t)MOST_PARTS * a.n_req * a.kv.kv_heads;
+  const int64_t piece = max(quotient(total + plan.waves - 1, plan.waves),
+                            quotient(total + at_most - 1, at_most));
   const int me = uni_int(block * ATT_WAVES + wave);
   const int64_t begin = me * piece;
   const int64_t end = min(total, begin + piece);

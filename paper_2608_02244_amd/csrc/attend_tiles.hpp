@@ -108,6 +108,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
   // LDS: K and V of two tiles, then a few words
   int(*reduce)[ATT_WAVES] = (int(*)[ATT_WAVES])(lds + 4 * L::BYTES);  // [2]
   int* found_tile = reduce[2];                                        // [2]
+  int* class_tiles = reduce[3];                                       // [8]
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 31, h = lane >> 5;
@@ -127,36 +128,66 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
     for (int i = tid; i <= a.n_req; i += ATT_THREADS) ints[i] = a.q_start[i];
     __syncthreads();
   } else {
-    // tiles of the requests before each: block-wide sums over all requests
+    // Which tile: those of the requests that see most keys go first (in eight classes by
+    // the keys that the request's last token sees), and in a request the last rows, so that
+    // the launch does not end with a few long tiles.
+    constexpr int CLASSES = 8;
     const int n = a.n_req, per = (n + ATT_THREADS - 1) / ATT_THREADS;
     const int r0 = min(n, tid * per), r1 = min(n, r0 + per);
-    auto tiles_of = [&](int i) {
+    auto tiles_of = [&](int i, int* work) {
       const Request y = request_of(a, i);
       const int rows = min(y.q_len, a.max_q) * a.group;
+      *work = a.window > 0 ? min(y.kv, a.window + min(a.n_sink, a.window)) : y.kv;
       return rows > plan.min_rows ? (rows + TILE_ROWS - 1) / TILE_ROWS : 0;
     };
+    int most = 0;
+    for (int i = r0; i < r1; ++i) {
+      int work;
+      if (tiles_of(i, &work) > 0) most = max(most, work);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) most = max(most, __shfl_xor(most, d));
+    if (lane == 0) reduce[0][wave] = most;
+    if (tid < CLASSES) class_tiles[tid] = 0;
+    __syncthreads();
+    most = max(max(reduce[0][0], reduce[0][1]), max(reduce[0][2], reduce[0][3]));
+    const float scale = (float)CLASSES / (float)(most + 1);
+    auto class_of = [&](int work) {  // 0: the most
+      return CLASSES - 1 - min(CLASSES - 1, (int)((float)work * scale));
+    };
+    for (int i = r0; i < r1; ++i) {
+      int work;
+      const int t = tiles_of(i, &work);
+      if (t > 0) atomicAdd(&class_tiles[class_of(work)], t);
+    }
+    __syncthreads();
+    int cls = 0;
+    while (cls < CLASSES && tile >= class_tiles[cls]) tile -= class_tiles[cls++];
+    if (cls == CLASSES) return;  // past the last
     int sum = 0;
-    for (int i = r0; i < r1; ++i) sum += tiles_of(i);
+    for (int i = r0; i < r1; ++i) {
+      int work;
+      const int t = tiles_of(i, &work);
+      if (t > 0 && class_of(work) == cls) sum += t;
+    }
     int s = sum;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int y = __shfl_up(s, d);
       if (lane >= d) s += y;
     }
-    if (lane == 63) reduce[0][wave] = s;
-    if (tid == 0) found_tile[0] = -1;
+    if (lane == 63) reduce[1][wave] = s;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) s += reduce[0][w];
-    const int all = reduce[0][0] + reduce[0][1] + reduce[0][2] + reduce[0][3];
-    if (tile >= all) return;
-    tile = all - 1 - tile;  // the last rows of a prompt see most keys: they go first
+    for (int w = 0; w < wave; ++w) s += reduce[1][w];
     int at = s - sum;
     if (tile >= at && tile < s) {
       for (int i = r0; i < r1; ++i) {
-        const int t = tiles_of(i);
+        int work;
+        const int t = tiles_of(i, &work);
+        if (t == 0 || class_of(work) != cls) continue;
         if (tile < at + t) {
           found_tile[0] = i;
-          found_tile[1] = tile - at;
+          found_tile[1] = t - 1 - (tile - at);
           break;
         }
         at += t;

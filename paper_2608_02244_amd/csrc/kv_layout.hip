@@ -22,25 +22,35 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int MAX_REQ = FSCHED_MAX_REQ;
+constexpr int MAX_BLOCKS = 512;  // more would only repeat the sums
 constexpr int TOK = 4;  // tokens per thread and turn: one 16-byte store each
 
 __device__ __forceinline__ int32_t sat32(int64_t x) {
   return x > INT_MAX ? INT_MAX : (int32_t)x;
 }
 
-// Inclusive sums of x over the block's threads (in thread order).
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* wave_sum) {
+// Sums of two values over the threads before the calling one, and over all.
+struct Sums {
+  int64_t a, b;
+};
+__device__ __forceinline__ Sums block_scan(int64_t a, int64_t b, Sums* wave_sum) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t x = a, y = b;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
+    const int64_t u = __shfl_up(x, d), v = __shfl_up(y, d);
+    if (lane >= d) {
+      x += u;
+      y += v;
+    }
   }
-  if (lane == 63) wave_sum[wave] = x;
+  if (lane == 63) wave_sum[wave] = Sums{x, y};
   __syncthreads();
-  for (int w = 0; w < wave; ++w) x += wave_sum[w];
-  __syncthreads();
-  return x;
+  for (int w = 0; w < wave; ++w) {
+    x += wave_sum[w].a;
+    y += wave_sum[w].b;
+  }
+  return Sums{x - a, y - b};
 }
 
 // Last r with start[r] <= x (start[0] = 0 <= x); requests without an element of
@@ -56,35 +66,36 @@ __device__ __forceinline__ int find(const int32_t* start, int n, int x) {
 }
 
 __global__ __launch_bounds__(THREADS) void kv_layout_kernel(LayoutArgs a) {
-  __shared__ int32_t tok0[MAX_REQ + 1], page0[MAX_REQ + 1];
-  __shared__ int64_t wave_sum[THREADS / 64];
+  // first token and first new page of every request, and what it held
+  __shared__ int32_t tok0[MAX_REQ + 1], page0[MAX_REQ + 1], held[MAX_REQ];
+  __shared__ Sums wave_sum[THREADS / 64];
   const int n = a.n_req;
   const int per = (n + THREADS - 1) / THREADS;
   const int r0 = min(n, (int)threadIdx.x * per), r1 = min(n, r0 + per);
   const int shift = a.page_shift;
   const int64_t page = 1ll << shift;
-
-  auto lens = [&](int r, int64_t* old_len, int64_t* add) {
-    *old_len = max(0, a.old_len[r]);
-    *add = max(0, a.new_len[r]);
-  };
   // pages of the first `len` tokens, as far as the table row goes
   auto pages_of = [&](int64_t len) { return min((len + page - 1) >> shift, (int64_t)a.width); };
 
   int64_t toks = 0, pages = 0;
   for (int r = r0; r < r1; ++r) {
-    int64_t o, m;
-    lens(r, &o, &m);
+    const int o = max(0, a.old_len[r]), m = max(0, a.new_len[r]);
+    held[r] = o;
+    tok0[r] = m;
     toks += m;
-    pages += pages_of(o + m) - pages_of(o);
+    pages += pages_of((int64_t)o + m) - pages_of(o);
   }
-  int64_t t = block_scan(toks, wave_sum) - toks;
-  int64_t g = block_scan(pages, wave_sum) - pages;
+  const Sums before = block_scan(toks, pages, wave_sum);
+  int64_t t = before.a, g = before.b;
+  const bool writes = blockIdx.x == 0;
   for (int r = r0; r < r1; ++r) {
-    int64_t o, m;
-    lens(r, &o, &m);
+    const int64_t o = held[r], m = tok0[r];
     tok0[r] = sat32(t);
     page0[r] = sat32(g);
+    if (writes) {
+      a.q_start[r] = (int)min(t, (int64_t)a.n_tok);
+      a.kv_len[r] = sat32(o + m);
+    }
     t += m;
     g += pages_of(o + m) - pages_of(o);
   }
@@ -92,28 +103,20 @@ __global__ __launch_bounds__(THREADS) void kv_layout_kernel(LayoutArgs a) {
   if (threadIdx.x == THREADS - 1) {
     tok0[n] = sat32(t);
     page0[n] = sat32(g);
+    if (writes) {
+      a.q_start[n] = (int)min(t, (int64_t)a.n_tok);
+      a.used[0] = sat32(g);
+      a.used[1] = sat32(t);
+    }
   }
   __syncthreads();
   const int all_tok = tok0[n], all_pages = page0[n];
   const int id = blockIdx.x * THREADS + threadIdx.x, step = gridDim.x * THREADS;
 
-  for (int r = id; r <= n; r += step) {
-    a.q_start[r] = min(tok0[r], a.n_tok);
-    if (r < n) {
-      int64_t o, m;
-      lens(r, &o, &m);
-      a.kv_len[r] = sat32(o + m);
-    }
-  }
-  if (id == 0) {
-    a.used[0] = all_pages;
-    a.used[1] = all_tok;
-  }
-
   // new pages: entry c of row r is free page page0[r] + c - have
   for (int64_t i = id; i < all_pages; i += step) {
     const int r = find(page0, n, (int)i);
-    const int64_t c = pages_of(max(0, a.old_len[r])) + (i - page0[r]);
+    const int64_t c = pages_of(held[r]) + (i - page0[r]);
     if (c < a.width) a.table[(int64_t)r * a.width + c] = i < a.n_free ? a.free_pages[i] : -1;
   }
 
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(THREADS) void kv_layout_kernel(LayoutArgs a) {
       slot[j] = pos[j] = -1;
       if (i >= limit) continue;
       while (tok0[r + 1] <= i) ++r;
-      const int64_t o = max(0, a.old_len[r]);
+      const int64_t o = held[r];
       const int64_t at = o + (i - tok0[r]);  // index in the request
       const int64_t c = at >> shift, have = pages_of(o);
       pos[j] = sat32(at + a.first_pos);
@@ -164,7 +167,7 @@ hipError_t launch_kv_layout(const LayoutArgs& a, hipStream_t s) {
   const int64_t per = THREADS * TOK;
   int64_t blocks = ((int64_t)a.n_tok + per - 1) / per;
   if (blocks < 1) blocks = 1;
-  if (blocks > 2048) blocks = 2048;
+  if (blocks > MAX_BLOCKS) blocks = MAX_BLOCKS;
   kv_layout_kernel<<<dim3((unsigned)blocks), dim3(THREADS), 0, s>>>(a);
   return hipGetLastError();
 }
