@@ -259,12 +259,12 @@ hipError_t launch_attend(const AttnArgs& a, int dtype, int head_dim, int n_cu, v
   const hipError_t e = dtype == FSCHED_BF16 ? main_launch<Bf16>(a, p.main, head_dim, s)
                                             : main_launch<F16>(a, p.main, head_dim, s);
   if (e != hipSuccess || !p.joins) return e;
-  // enough blocks to fill the device, of at most 64 rows and at least one
+  // enough blocks to fill the device, of 4 to 64 rows each
   const int64_t most = p.join.own_split + p.join.pre_split > 0 ? (int64_t)a.max_q * a.q_heads
                                                                : p.join.slot_rows * a.kv.kv_heads;
   int64_t y = (8 * n_cu + a.n_req - 1) / a.n_req;
+  if (y > most / 4) y = most / 4;
   if (y < most / 64) y = most / 64;
-  if (y > most) y = most;
   if (y > 1024) y = 1024;
   if (y < 1) y = 1;
   const dim3 grid((unsigned)a.n_req, (unsigned)y);
