@@ -1,7 +1,9 @@
 """Build libfsched.so in-tree with hipcc for gfx950.
 
 Every HIP translation unit under csrc/ is compiled in parallel, then linked
-into one shared library next to this file.  No CPU fallback is built.
+into one shared library next to this file; the binding of the step's operators
+(csrc/bind) becomes an extension module beside it, compiled against torch.  No CPU
+fallback is built.
 """
 from __future__ import annotations
 
@@ -17,6 +19,8 @@ CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libfsched.so")
+BIND_SRC = os.path.join(CSRC, "bind", "step_bind.cpp")
+BIND_LIB = os.path.join(HERE, "_step.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 
 ARCH = "gfx950"
@@ -51,10 +55,41 @@ def _compile(src: str) -> str:
     obj = os.path.join(BUILD_DIR, os.path.basename(src) + ".o")
     lang = ["-x", "hip"] if src.endswith(".hip") else []
     cmd = [_hipcc()] + COMMON + _flags(src) + lang + ["-c", src, "-o", obj]
+    _run(cmd, "compile")
+    return obj
+
+
+def _run(cmd: list, what: str) -> None:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+        raise RuntimeError(f"{what} failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+
+
+def _compile_bind() -> str:
+    """Object file of the binding (host code only)."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    obj = os.path.join(BUILD_DIR, "step_bind.o")
+    cxx = shutil.which("g++") or "c++"
+    inc = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], INCLUDE]
+    _run([cxx, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
+         [f"-I{p}" for p in inc] + ["-c", BIND_SRC, "-o", obj], "compile")
     return obj
+
+
+def _link_bind(obj: str) -> None:
+    """The extension module, which finds libfsched.so beside it (torch's libraries are
+    loaded by the time it is imported)."""
+    from torch.utils import cpp_extension
+    cxx = shutil.which("g++") or "c++"
+    lib = cpp_extension.library_paths()[0]
+    tmp = BIND_LIB + ".tmp"
+    _run([cxx, "-shared", "-o", tmp, obj, f"-L{HERE}", "-lfsched", f"-L{lib}", "-lc10",
+          "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"], "link")
+    os.replace(tmp, BIND_LIB)
 
 
 def build(jobs: int | None = None, verbose: bool = False) -> str:
@@ -62,13 +97,14 @@ def build(jobs: int | None = None, verbose: bool = False) -> str:
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.cpp")))
     jobs = jobs or min(len(srcs), os.cpu_count() or 4, 16)
     with cf.ThreadPoolExecutor(max_workers=jobs) as ex:
+        bind = ex.submit(_compile_bind)
         objs = list(ex.map(_compile, srcs))
+        bind_obj = bind.result()
     tmp = LIB + ".tmp"
     cmd = [_hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + objs
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    _run(cmd, "link")
     os.replace(tmp, LIB)
+    _link_bind(bind_obj)
     if verbose:
         print(f"built {LIB}")
     return LIB
