@@ -186,11 +186,11 @@ Shape plan(const AttnArgs& a, int head_dim, int n_cu, char* ws) {
     p.join.tiles = rp.tiles;
   }
   // Keys are cut so that the places beside the rows blocks have work, none fewer than
-  // 256 keys: parts cost their bytes twice.
+  // 128 keys: parts cost their bytes twice.
   const int64_t places = (with_rows ? 1 : 2) * (int64_t)n_cu;
   auto cut = [&](int64_t tiles, int64_t keys) {
     const int64_t want = (places + tiles * a.kv.kv_heads - 1) / (tiles * a.kv.kv_heads);
-    const int64_t can = keys / 256 > 1 ? keys / 256 : 1;
+    const int64_t can = keys / 128 > 1 ? keys / 128 : 1;
     const int64_t s = want < can ? want : can;
     return (int)(s < 1 ? 1 : s);
   };

@@ -63,7 +63,8 @@ template <class T, int D, int RT>
 hipError_t launch_main_rows(const AttnArgs& a, const MainPlan& p, hipStream_t s) {
   const bool tiles = p.pre_blocks + p.own_blocks > 0, wide = a.kv.page_shift >= WIDE_SHIFT;
   const dim3 grid((unsigned)(p.rows_blocks + p.pre_blocks + p.own_blocks)), block(ATT_THREADS);
-  const size_t rl = rows_lds(a.n_req), lds = tiles && rl < tiles_lds<D>() ? tiles_lds<D>() : rl;
+  const size_t rl = rows_lds(a.n_req), tl = tiles_lds<D>(p.pre_blocks > 0, a.n_req);
+  const size_t lds = tiles && rl < tl ? tl : rl;
   void (*kernel)(AttnArgs, MainPlan) =
       tiles ? (wide ? attend_both_kernel<T, D, RT, true> : attend_both_kernel<T, D, RT, false>)
             : (wide ? attend_rows_kernel<T, D, RT, true> : attend_rows_kernel<T, D, RT, false>);
@@ -79,7 +80,7 @@ hipError_t launch_main(const AttnArgs& a, const MainPlan& p, hipStream_t s) {
     return launch_main_rows<T, D, 1>(a, p, s);
   }
   const dim3 grid((unsigned)(p.pre_blocks + p.own_blocks)), block(ATT_THREADS);
-  const size_t lds = tiles_lds<D>();
+  const size_t lds = tiles_lds<D>(p.pre_blocks > 0, a.n_req);
   void (*kernel)(AttnArgs, MainPlan) = a.kv.page_shift >= WIDE_SHIFT
                                            ? attend_tiles_kernel<T, D, true>
                                            : attend_tiles_kernel<T, D, false>;

@@ -111,13 +111,14 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const RowsPlan& p
   auto quotient = [](int64_t x, int64_t y) {  // a 64-bit division is some 130 instructions
     return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
   };
-  // a few tiles are not cut finer than their parts are worth reading again
-  const int64_t at_most = (int64_t)MOST_PARTS * a.n_req * a.kv.kv_heads;
-  const int64_t piece = max(quotient(total + plan.waves - 1, plan.waves),
-                            quotient(total + at_most - 1, at_most));
+  // Waves with work: a few tiles are not cut finer than their parts are worth reading
+  // again.  Wave i takes units i total / waves .. (i + 1) total / waves.
+  const int64_t waves = min(min((int64_t)plan.waves, total),
+                            (int64_t)MOST_PARTS * a.n_req * a.kv.kv_heads);
   const int me = uni_int(block * ATT_WAVES + wave);
-  const int64_t begin = me * piece;
-  const int64_t end = min(total, begin + piece);
+  if (me >= waves) return;
+  const int64_t begin = quotient(me * total, waves), end = quotient((me + 1) * total, waves);
+  auto wave_of = [&](int64_t unit) { return (int)quotient((unit + 1) * waves - 1, total); };
 
   for (int64_t w = begin; w < end;) {
     const int kh = (int)quotient(w, per_head);
@@ -328,7 +329,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const RowsPlan& p
       RowsTile d;
       d.first = slot;
       d.wave = me;
-      d.count = (int)quotient(w + units - 1, piece) - me + 1;
+      d.count = wave_of(w + units - 1) - me + 1;
       d.pad = 0;
       plan.tiles[(int64_t)kh * a.n_req + r] = d;
     }

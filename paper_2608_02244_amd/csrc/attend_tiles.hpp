@@ -109,6 +109,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
   int(*reduce)[ATT_WAVES] = (int(*)[ATT_WAVES])(lds + 4 * L::BYTES);  // [2]
   int* found_tile = reduce[2];                                        // [2]
   int* class_tiles = reduce[3];                                       // [8]
+  int32_t* starts = (int32_t*)(lds + 4 * L::BYTES + 256);             // [n_req + 1], prefix only
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 31, h = lane >> 5;
@@ -119,14 +120,80 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
   const int part = id % plan.split;
   int tile = id / plan.split;
 
+  const int offset = plan.prefix ? 0 : a.prefix_len;  // position of key 0
+  const int sink_keys = a.window > 0 ? a.n_sink - offset : 0;
+  const int32_t* table = a.prefix_pages;  // own keys: set once the request is known
+  // The keys that the block's rows see: n_keys and tiles b0 .. b1 of span sp.
+  int n_keys = 0, b0 = 0, b1 = 0, bmin = 0;
+  Span sp = {0, 0, 0};
+  auto cut = [&]() {
+    b0 = (int)((int64_t)sp.blocks * part / plan.split);
+    b1 = (int)((int64_t)sp.blocks * (part + 1) / plan.split);
+  };
+  // LDS places: buffer b holds K at 2 b BYTES, V behind it
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const char* kbase = (const char*)((const elem*)a.kv.k + kh * a.kv.k_head);
+  const char* vbase = (const char*)((const elem*)a.kv.v + kh * a.kv.v_head);
+  const uint32_t k_slot = (uint32_t)a.kv.k_slot * 2, v_slot = (uint32_t)a.kv.v_slot * 2;
+  // Key (lane mod KB) of tile b: whether some row of the block sees it, and its page (for
+  // keys past the last one the last one's); looked at only when its turn comes.
+  auto key_at = [&](int b) { return sp.block(b) * KB + (lane & (KB - 1)); };
+  auto seen = [&](int s) {
+    return s < n_keys && (a.window == 0 || s > bmin - a.window || s < sink_keys);
+  };
+  auto page_at = [&](int b) { return table[min(key_at(b), n_keys - 1) >> shift]; };
+  auto in_cache = [&](int page) { return (uint32_t)page < (uint32_t)a.kv.n_pages; };
+  // tile b to buffer `buf`; keys that are not in the cache read page 0 (they are masked).
+  // A lane computes the addresses of key (lane mod KB), and the loads take them from there.
+  auto fetch = [&](int b, int page, int buf) {
+    constexpr int AT_ONCE = ATT_THREADS / L::PIECES, PER_WAVE = 64 / L::PIECES;
+    const uint32_t pg = in_cache(page) ? page : 0, slot = key_at(b) & page_mask;
+    const uint64_t k_from = (uint64_t)kbase + pg * (uint64_t)(a.kv.k_page * 2) + slot * k_slot;
+    const uint64_t v_from = (uint64_t)vbase + pg * (uint64_t)(a.kv.v_page * 2) + slot * v_slot;
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+      const uint32_t to = uni_int(lds0 + buf * (2 * L::BYTES) + (i * ATT_THREADS + wave * 64) * 16);
+      const int key = i * AT_ONCE + tid / L::PIECES;
+      const uint32_t piece = ((tid % L::PIECES) ^ L::swizzle(key)) * 16;
+      if constexpr (WIDE) {
+        const int first = uni_int(i * AT_ONCE + wave * PER_WAVE);
+        const uint32_t mine = lane / L::PIECES;
+        load_to_lds((const char*)lane_of(k_from, first), mine * k_slot + piece, to);
+        load_to_lds((const char*)lane_of(v_from, first), mine * v_slot + piece, to + L::BYTES);
+      } else {
+        load_to_lds((const char*)shuffled(k_from, key) + piece, to);
+        load_to_lds((const char*)shuffled(v_from, key) + piece, to + L::BYTES);
+      }
+    }
+  };
+
+  int page = 0, page_next = 0;
+  auto first_fetch = [&]() {
+    if (b0 >= b1) return;
+    page = page_at(b0);
+    fetch(b0, page, 0);
+    if (b0 + 1 < b1) page_next = page_at(b0 + 1);
+  };
+  // Without a window a prefix's keys do not depend on the rows: the first tile is on its
+  // way before the rows' requests are looked up.  (A request with fewer own tokens than new
+  // ones has rows that see less of it; the mask says so.)
+  const bool early = plan.prefix && a.window == 0 && a.kv.n_pages > 0;
+  if (plan.prefix) {
+    if (early) {
+      n_keys = a.prefix_len;
+      sp.blocks = (n_keys + KB - 1) / KB;
+      cut();
+      first_fetch();
+    }
+    for (int i = tid; i <= a.n_req; i += ATT_THREADS) starts[i] = a.q_start[i];
+  }
+
   // which rows: `tok` and `top` (index of the last key that it sees) of this lane's
   Request x;
   int r = 0, row0;  // row0: the block's first row among the request's (the step's) rows
-  int32_t* ints = (int32_t*)lds;
   if (plan.prefix) {
     row0 = tile * TILE_ROWS;
-    for (int i = tid; i <= a.n_req; i += ATT_THREADS) ints[i] = a.q_start[i];
-    __syncthreads();
+    __syncthreads();  // the starts are in LDS
   } else {
     // Which tile: those of the requests that see most keys go first (in eight classes by
     // the keys that the request's last token sees), and in a request the last rows, so that
@@ -197,6 +264,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
     r = found_tile[0];
     row0 = found_tile[1] * TILE_ROWS;
     x = request_of(a, r);
+    table = a.table + (int64_t)r * a.width;
   }
 
   int tok = 0, top = -1, qh = kh * a.group;
@@ -211,7 +279,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
         int lo = 0, hi = a.n_req;
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
-          if (ints[mid] <= i) lo = mid;
+          if (starts[mid] <= i) lo = mid;
           else hi = mid;
         }
         const Request y = request_of(a, lo);
@@ -227,8 +295,6 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
     if (on) qh += g;
   }
   const int n_held = plan.prefix ? a.prefix_len : x.kv;
-  const int offset = plan.prefix ? 0 : a.prefix_len;
-  const int sink_keys = a.window > 0 ? a.n_sink - offset : 0;
   const int low = a.window > 0 ? top - a.window : -0x7fffffff - 1;
   // first and last key index of the wave's rows, and of the block's
   int wmin = on ? top : 0x7fffffff, wmax = on ? top : -0x7fffffff;
@@ -237,23 +303,26 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
     wmin = min(wmin, __shfl_xor(wmin, d));
     wmax = max(wmax, __shfl_xor(wmax, d));
   }
-  __syncthreads();  // ints and reduce are read
+  __syncthreads();  // reduce is read
   if (lane == 0) {
     reduce[0][wave] = wmin;
     reduce[1][wave] = wmax;
   }
   __syncthreads();
-  const int bmin = min(min(reduce[0][0], reduce[0][1]), min(reduce[0][2], reduce[0][3]));
+  bmin = min(min(reduce[0][0], reduce[0][1]), min(reduce[0][2], reduce[0][3]));
   const int bmax = max(max(reduce[1][0], reduce[1][1]), max(reduce[1][2], reduce[1][3]));
   wmin = uni_int(wmin);
   wmax = uni_int(wmax);
 
   // this part's tiles of keys
-  const int n_keys = max(0, min(n_held, bmax + 1));
-  Span sp = span_of<KB>(bmin, bmax, n_keys, a.window, a.n_sink, offset);
-  if (bmax < 0 || a.kv.n_pages == 0) sp.blocks = 0;
-  const int b0 = (int)((int64_t)sp.blocks * part / plan.split);
-  const int b1 = (int)((int64_t)sp.blocks * (part + 1) / plan.split);
+  if (!early) {
+    n_keys = max(0, min(n_held, bmax + 1));
+    sp = span_of<KB>(bmin, bmax, n_keys, a.window, a.n_sink, offset);
+    if (bmax < 0 || a.kv.n_pages == 0) sp.blocks = 0;
+    cut();
+  }
+
+  if (!early) first_fetch();
 
   x8 q[QC];
   {
@@ -269,8 +338,6 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
     for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
   float mu = NEG_INF, l = 0.0f;
 
-  // LDS places: buffer b holds K at 2 b BYTES, V behind it
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int f = L::swizzle(col);
   uint32_t k_at[QC];  // key `col`, piece 2c + h
 #pragma unroll
@@ -286,48 +353,6 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
       v_at[xx][d] = lds0 + L::BYTES + key * (D * 2) + (piece ^ L::swizzle(key)) * 16 + (e & 1) * 8;
     }
 
-  const int32_t* table = plan.prefix ? a.prefix_pages : a.table + (int64_t)r * a.width;
-  const char* kbase = (const char*)((const elem*)a.kv.k + kh * a.kv.k_head);
-  const char* vbase = (const char*)((const elem*)a.kv.v + kh * a.kv.v_head);
-  const uint32_t k_slot = (uint32_t)a.kv.k_slot * 2, v_slot = (uint32_t)a.kv.v_slot * 2;
-  // Key (lane mod KB) of tile b: whether some row of the block sees it, and its page (for
-  // keys past the last one the last one's); looked at only when its turn comes.
-  auto key_at = [&](int b) { return sp.block(b) * KB + (lane & (KB - 1)); };
-  auto seen = [&](int s) {
-    return s < n_keys && (a.window == 0 || s > bmin - a.window || s < sink_keys);
-  };
-  auto page_at = [&](int b) { return table[min(key_at(b), n_keys - 1) >> shift]; };
-  auto in_cache = [&](int page) { return (uint32_t)page < (uint32_t)a.kv.n_pages; };
-  // tile b to buffer `buf`; keys that are not in the cache read page 0 (they are masked).
-  // A lane computes the addresses of key (lane mod KB), and the loads take them from there.
-  auto fetch = [&](int b, int page, int buf) {
-    constexpr int AT_ONCE = ATT_THREADS / L::PIECES, PER_WAVE = 64 / L::PIECES;
-    const uint32_t pg = in_cache(page) ? page : 0, slot = key_at(b) & page_mask;
-    const uint64_t k_from = (uint64_t)kbase + pg * (uint64_t)(a.kv.k_page * 2) + slot * k_slot;
-    const uint64_t v_from = (uint64_t)vbase + pg * (uint64_t)(a.kv.v_page * 2) + slot * v_slot;
-#pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-      const uint32_t to = uni_int(lds0 + buf * (2 * L::BYTES) + (i * ATT_THREADS + wave * 64) * 16);
-      const int key = i * AT_ONCE + tid / L::PIECES;
-      const uint32_t piece = ((tid % L::PIECES) ^ L::swizzle(key)) * 16;
-      if constexpr (WIDE) {
-        const int first = uni_int(i * AT_ONCE + wave * PER_WAVE);
-        const uint32_t mine = lane / L::PIECES;
-        load_to_lds((const char*)lane_of(k_from, first), mine * k_slot + piece, to);
-        load_to_lds((const char*)lane_of(v_from, first), mine * v_slot + piece, to + L::BYTES);
-      } else {
-        load_to_lds((const char*)shuffled(k_from, key) + piece, to);
-        load_to_lds((const char*)shuffled(v_from, key) + piece, to + L::BYTES);
-      }
-    }
-  };
-
-  int page = 0, page_next = 0;
-  if (b0 < b1) {
-    page = page_at(b0);
-    fetch(b0, page, 0);
-    if (b0 + 1 < b1) page_next = page_at(b0 + 1);
-  }
   for (int b = b0; b < b1; ++b) {
     const int buf = (b - b0) & 1;
     wait_loads();
@@ -476,8 +501,8 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
 }
 
 template <int D>
-constexpr size_t tiles_lds() {
-  return 4 * (size_t)Tile<D>::BYTES + 256;
+inline size_t tiles_lds(bool prefix, int n_req) {
+  return 4 * (size_t)Tile<D>::BYTES + 256 + (prefix ? (size_t)(n_req + 1) * sizeof(int32_t) : 0);
 }
 
 }  // namespace fs
