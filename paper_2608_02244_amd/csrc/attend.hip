@@ -170,12 +170,12 @@ Shape plan(const AttnArgs& a, int head_dim, int n_cu, char* ws) {
     // beside tiles blocks one rows block per compute unit, else as many as fit
     p.main.rows_blocks = with_tiles || prefix
                              ? n_cu
-                             : n_cu * rows_occupancy(head_dim, rp.row_tiles,
-                                                     a.kv.page_shift >= WIDE_SHIFT);
+                             : n_cu * rows_occupancy(head_dim);
     rp.waves = p.main.rows_blocks * ATT_WAVES;
     rp.keep_parts = prefix;
     rp.slot_rows = most < limit ? (int)most : limit;
-    const size_t slots = 2 * (size_t)rp.waves * rp.slot_rows;
+    const size_t whole = prefix ? (size_t)a.n_req * a.kv.kv_heads : 0;
+    const size_t slots = (2 * (size_t)rp.waves + whole) * rp.slot_rows;
     rp.part_o = (float*)take(slots * head_dim * sizeof(float));
     rp.part_ml = (float2*)take(slots * sizeof(float2));
     rp.tiles = (RowsTile*)take((size_t)a.n_req * a.kv.kv_heads * sizeof(RowsTile));

@@ -18,7 +18,7 @@ struct MainPlan {
 };
 
 template <class T, int D, int RT, bool WIDE>
-__global__ __launch_bounds__(ATT_THREADS, rows_occupancy(D, RT, WIDE)) void attend_rows_kernel(
+__global__ __launch_bounds__(ATT_THREADS, rows_occupancy(D)) void attend_rows_kernel(
     AttnArgs a, MainPlan p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   attend_rows<T, D, RT, WIDE>(a, p.rows, blockIdx.x, lds);

@@ -17,7 +17,9 @@
 // spreads over the device.  A wave works alone (no barrier, nothing shared after the
 // first sums), so while one changes tiles the others of its unit keep loads in flight.
 // Pieces that cover a whole tile write its result; the others write parts, which a
-// second launch joins.
+// second launch joins.  A wave has two parts at most, the tiles at its piece's ends;
+// behind a shared prefix, where whole tiles are parts too and a piece may hold any
+// number of them, those have a slot of their own per tile.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -29,7 +31,7 @@ namespace fs {
 struct RowsTile {
   int32_t first;  // slot of its first part
   int32_t wave;   // wave that wrote it; the others are slots 2 (wave + 1), 2 (wave + 2), ..
-  int32_t count;  // parts; 1: the wave wrote the result itself
+  int32_t count;  // parts; 1: a whole tile (the result itself unless keep_parts)
   int32_t pad;
 };
 
@@ -38,8 +40,9 @@ struct RowsPlan {
   int32_t row_tiles;    // 16-row tiles of a request and key head (1 or 2)
   int32_t slot_rows;    // rows of a part's slot
   int32_t keep_parts;   // 1: results join with those of the prefix, written as parts
-  float* part_o;        // [2 * waves][slot_rows][head_dim]
-  float2* part_ml;      // [2 * waves][slot_rows] (mu, l)
+  float* part_o;        // [slots][slot_rows][head_dim]; slots: 2 per wave, then with
+                        // keep_parts one per tile, for those that lie in one piece
+  float2* part_ml;      // [slots][slot_rows] (mu, l)
   RowsTile* tiles;      // [kv_heads][n_req]
 };
 
@@ -47,9 +50,7 @@ constexpr int UNIT = 32;       // keys of a unit
 constexpr int MOST_PARTS = 32;  // of a tile, on average
 
 // Blocks per compute unit that the registers allow.
-constexpr int rows_occupancy(int D, int RT, bool wide) {
-  return D == 64 ? 3 : 2;
-}
+constexpr int rows_occupancy(int D) { return D == 64 ? 3 : 2; }
 
 // WIDE: pages of 16 tokens and more, so that keys 0..15 and 16..31 of a unit lie in
 // one page each and their addresses are uniform but for a lane's constant offset.
@@ -324,14 +325,16 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const RowsPlan& p
     }
 
     const bool whole = u0 == 0 && u1 == units;
-    const int slot = 2 * me + (w != begin);
+    const int64_t tile = (int64_t)kh * a.n_req + r;
+    const int64_t slot =
+        whole && plan.keep_parts ? 2 * (int64_t)plan.waves + tile : 2 * (int64_t)me + (w != begin);
     if (u0 == 0 && lane == 0) {
       RowsTile d;
-      d.first = slot;
+      d.first = (int32_t)slot;
       d.wave = me;
       d.count = wave_of(w + units - 1) - me + 1;
       d.pad = 0;
-      plan.tiles[(int64_t)kh * a.n_req + r] = d;
+      plan.tiles[tile] = d;
     }
     // a lane holds 4 DL neighbouring elements of its row, from 4 DL h on
 #pragma unroll
@@ -356,7 +359,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const RowsPlan& p
         if (a.lse && h == 0)
           a.lse[(int64_t)(x.q0 + tok) * a.q_heads + qh] = (mu[t] + log2f(sum)) * LN2;
       } else {
-        const int64_t at = (int64_t)slot * plan.slot_rows + row;
+        const int64_t at = slot * plan.slot_rows + row;
         float* dst = plan.part_o + at * D + 4 * DL * h;
 #pragma unroll
         for (int i = 0; i < 4; ++i)

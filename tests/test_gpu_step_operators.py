@@ -501,6 +501,14 @@ def test_shared_prefix_many_rows_and_one_request(dev):
     Batch(dev, [1, 3], [0, 2], 8, 2, 128, prefix=40).check()  # fewer own tokens than new ones
 
 
+@pytest.mark.parametrize("n,heads,D", [(300, (8, 8), 64), (170, (16, 16), 128)])
+def test_shared_prefix_more_requests_than_waves(dev, n, heads, D):
+    """Own parts so short and many that a wave works on several requests in a row."""
+    Batch(dev, [1] * n, [1 + 7 * i % 39 for i in range(n)], *heads, D, prefix=33, seed=n).check()
+    Batch(dev, [1 + i % 2 for i in range(n)], [2 + 11 * i % 71 for i in range(n)], *heads, D,
+          prefix=18, seed=n).check()
+
+
 def test_attend_peaked_and_flat_scores(dev):
     """Scores whose weights span the type's range, both ways."""
     for spread in (0.0, 0.01, 30.0):
