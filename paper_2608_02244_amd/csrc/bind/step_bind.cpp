@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -27,6 +28,21 @@ std::string dtype_name(at::ScalarType t) {
 const at::Tensor& tensor(PyObject* o, const char* name) {
   if (!THPVariable_Check(o)) throw Refused{std::string(name) + " must be a tensor"};
   return THPVariable_Unpack(o);
+}
+
+// The tensors among a call's arguments lie on one device, which is current during the
+// call (kernels read all of them, and the library launches on the current device).
+c10::DeviceGuard one_device(PyObject* const* a, Py_ssize_t n) {
+  const at::Tensor* first = nullptr;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (!THPVariable_Check(a[i])) continue;
+    const at::Tensor& t = THPVariable_Unpack(a[i]);
+    if (!first) first = &t;
+    else if (t.device() != first->device())
+      throw Refused{"all tensors of a call must be on one GPU"};
+  }
+  if (!first) throw Refused{"the first argument must be a GPU tensor"};
+  return c10::DeviceGuard(first->device());
 }
 
 int64_t integer(PyObject* o, int64_t lo, int64_t hi, const char* name) {
@@ -148,6 +164,8 @@ PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F body) {
     PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {
+    PyErr_SetString(PyExc_RuntimeError, "unknown C++ exception");
   }
   return nullptr;
 }
@@ -159,6 +177,7 @@ at::TensorOptions like(const at::Tensor& t, at::ScalarType type) {
 // (old_len, new_len, block_table, free_pages, page_size, n_tok, first_pos, stream)
 PyObject* kv_layout(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded(n_args, 8, [&]() -> PyObject* {
+    const c10::DeviceGuard on = one_device(a, n_args);
     const at::Tensor& old_len = tensor(a[0], "old_len");
     const int64_t n = old_len.dim() == 1 ? old_len.size(0) : -1;
     fsched_layout_params p{};
@@ -201,6 +220,7 @@ PyObject* kv_layout(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 //  interleaved, out, stream)
 PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded(n_args, 12, [&]() -> PyObject* {
+    const c10::DeviceGuard on = one_device(a, n_args);
     const Cache c = cache(a[4], a[5]);
     const int64_t dim = c.c.head_dim;
     const at::Tensor& qkv = rows(a[0], 3, c.type, "qkv");
@@ -255,10 +275,11 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 }
 
 // (q, k_cache, v_cache, prefix_pages, prefix_len, block_table, q_start, kv_len, scale,
-//  window, n_sink, max_q, out, return_lse, workspace, own_workspace, stream)
-// prefix_pages None: fsched_attend.  own_workspace: take one from torch's allocator.
+//  window, n_sink, max_q, out, return_lse, workspace, stream)
+// prefix_pages None: fsched_attend.  workspace None: taken from torch's allocator.
 PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
-  return guarded(n_args, 17, [&]() -> PyObject* {
+  return guarded(n_args, 16, [&]() -> PyObject* {
+    const c10::DeviceGuard on = one_device(a, n_args);
     const bool shared = a[3] != Py_None;
     const char* name = shared ? "fsched_attend_shared" : "fsched_attend";
     const Cache c = cache(a[1], a[2]);
@@ -298,12 +319,12 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       workspace = tensor(a[14], "workspace");
       if (!workspace.is_cuda() || !workspace.is_contiguous())
         throw Refused{"workspace must be a contiguous GPU tensor"};
-    } else if (truth(a[15])) {
+    } else {
       int64_t need = 0;
       check(fsched_attend_workspace(&p, &c.c, &need), name);
       if (need > 0) workspace = at::empty({need}, like(q, at::kByte));
     }
-    void* stream = handle(a[16]);
+    void* stream = handle(a[15]);
     const void* q_p = q.data_ptr();
     void* out_p = out.data_ptr();
     float* lse_p = lse.defined() ? (float*)lse.data_ptr() : nullptr;

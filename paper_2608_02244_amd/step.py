@@ -3,8 +3,13 @@ keys with the store into the cache, and attention over the paged cache.
 
 Binding of ``fsched_kv_layout``, ``fsched_qk_norm_rope``, ``fsched_attend`` and
 ``fsched_attend_shared`` (``include/fsched.h`` says what each computes).  Every
-array is a torch tensor on the GPU, the calls are enqueued on the current torch
-stream (or ``stream``) and nothing is synchronised.
+array is a torch tensor, all of a call's on one GPU; the calls are enqueued on the
+current torch stream and nothing is synchronised.  They are for serving: no gradient
+flows through them.
+
+With ``stream`` (a torch.cuda.Stream) a call runs as under ``torch.cuda.stream``: its
+outputs and workspace are allocated for that stream, and the caller orders the
+streams (inputs written on another one; results read on another one).
 
 A cache is a pair of tensors [n_pages, kv_heads, page_size, head_dim]; a permuted
 view (another order of page, head and slot in memory) does as well, as long as the
@@ -54,10 +59,8 @@ class AttnParams(ctypes.Structure):
          ("out_token_stride", _I64), ("out_head_stride", _I64)]
 
 
-def _stream(stream, x):
-    """Address of a stream: the given one's, else that of torch's current one."""
-    if stream is not None:
-        return stream.cuda_stream
+def _current(x):
+    """Address of torch's current stream."""
     return torch._C._cuda_getCurrentRawStream(x.get_device()) if x.is_cuda else 0
 
 
@@ -67,8 +70,12 @@ def kv_layout(old_len, new_len, block_table, free_pages, *, page_size: int, n_to
 
     ``block_table`` [n_req, width] is updated in place.  Returns (slots [n_tok],
     positions [n_tok], q_start [n_req + 1], kv_len [n_req], used [2]), int32."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return kv_layout(old_len, new_len, block_table, free_pages, page_size=page_size,
+                             n_tok=n_tok, first_pos=first_pos)
     return _step.kv_layout(old_len, new_len, block_table, free_pages, page_size, n_tok, first_pos,
-                           _stream(stream, old_len))
+                           _current(old_len))
 
 
 def qk_norm_rope(qkv, positions, slots, cos_sin, k_cache, v_cache, q_weight=None, k_weight=None,
@@ -77,8 +84,12 @@ def qk_norm_rope(qkv, positions, slots, cos_sin, k_cache, v_cache, q_weight=None
     rotated queries [n_tok, q_heads, head_dim] (``out``, made if None), keys and
     values put into the caches at ``slots`` (None: nowhere).  ``cos_sin`` [n_pos,
     rot_dim] f32 (None: no rotation, ``positions`` may be None)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return qk_norm_rope(qkv, positions, slots, cos_sin, k_cache, v_cache, q_weight,
+                                k_weight, eps=eps, interleaved=interleaved, out=out)
     return _step.qk_norm_rope(qkv, positions, slots, cos_sin, k_cache, v_cache, q_weight,
-                              k_weight, eps, interleaved, out, _stream(stream, qkv))
+                              k_weight, eps, interleaved, out, _current(qkv))
 
 
 def attend(q, k_cache, v_cache, block_table, q_start, kv_len, *, scale=None, window: int = 0,
@@ -92,11 +103,15 @@ def attend(q, k_cache, v_cache, block_table, q_start, kv_len, *, scale=None, win
     ``n_sink``.  ``max_q``: no request has more new tokens (1 for a decode step; None:
     not known).  ``scale`` None: head_dim ** -0.5.  ``workspace``: a GPU tensor of
     ``attend_workspace`` bytes, for calls that may not allocate.  None: taken from
-    torch's allocator (with ``stream`` given: from the library's pool).
+    torch's allocator.
     Returns out, or (out, lse [n_tok, q_heads] float32) with ``return_lse``."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return attend(q, k_cache, v_cache, block_table, q_start, kv_len,
+                          scale=scale, window=window, n_sink=n_sink, max_q=max_q, out=out,
+                          return_lse=return_lse, workspace=workspace)
     return _step.attend(q, k_cache, v_cache, None, 0, block_table, q_start, kv_len, scale, window,
-                        n_sink, max_q, out, return_lse, workspace, stream is None,
-                        _stream(stream, q))
+                        n_sink, max_q, out, return_lse, workspace, _current(q))
 
 
 def attend_shared(q, k_cache, v_cache, prefix_pages, prefix_len: int, block_table, q_start,
@@ -105,9 +120,15 @@ def attend_shared(q, k_cache, v_cache, prefix_pages, prefix_len: int, block_tabl
     """fsched_attend_shared: ``attend`` for requests that all begin with the
     ``prefix_len`` tokens held in ``prefix_pages``; ``block_table`` and ``kv_len``
     describe each request's own tokens behind them."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return attend_shared(q, k_cache, v_cache, prefix_pages, prefix_len, block_table,
+                                 q_start, kv_len, scale=scale, window=window, n_sink=n_sink,
+                                 max_q=max_q, out=out, return_lse=return_lse,
+                                 workspace=workspace)
     return _step.attend(q, k_cache, v_cache, prefix_pages, prefix_len, block_table, q_start,
                         kv_len, scale, window, n_sink, max_q, out, return_lse, workspace,
-                        stream is None, _stream(stream, q))
+                        _current(q))
 
 
 def attend_workspace(n_tok: int, n_req: int, q_heads: int, kv_heads: int, head_dim: int, *,

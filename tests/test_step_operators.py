@@ -207,6 +207,16 @@ def test_binding_refuses_what_is_not_on_the_gpu():
         fs.attend(x, kv.float(), kv.float(), i.view(4, 1), i, i)
 
 
+def test_binding_refuses_tensors_of_several_devices():
+    import torch
+    i = torch.zeros(4, dtype=torch.int32)
+    m = torch.zeros(4, 1, dtype=torch.int32, device="meta")
+    with pytest.raises(ValueError, match="one GPU"):
+        fs.kv_layout(i, i, m, i, page_size=16, n_tok=4)
+    with pytest.raises(ValueError, match="one GPU"):
+        fs.attend(m, m, m, i.view(4, 1), i, i)
+
+
 def test_package_still_loads_without_torch_in_hand():
     """The evaluation calls work on numpy arrays alone: importing the package and its
     step binding loads no torch."""
