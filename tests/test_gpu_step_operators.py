@@ -658,3 +658,84 @@ def test_step_in_a_captured_graph(dev):
         b = one()
         torch.cuda.synchronize()
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_given_stream_runs_there_and_owns_its_outputs(dev):
+    import torch
+    b = Batch(dev, [1, 40, 1], [70, 90, 33], 8, 2, 64)
+    out, lse = b.call()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got, got_lse = b.call(stream=s)
+    s.synchronize()
+    assert torch.equal(out, got) and torch.equal(lse, got_lse)
+    at = got.data_ptr()
+    del got
+    with torch.cuda.stream(s):  # its memory went back to the stream that it was made for
+        assert torch.empty_like(out).data_ptr() == at
+    lens = torch.tensor([1, 2], dtype=torch.int32, device=dev)
+    table = torch.full((2, 3), -1, dtype=torch.int32, device=dev)
+    free = torch.arange(6, dtype=torch.int32, device=dev)
+    s.wait_stream(torch.cuda.current_stream())
+    got = fs.kv_layout(lens * 0, lens, table, free, page_size=16, n_tok=3, stream=s)
+    s.synchronize()
+    assert got[0].tolist() == [0, 16, 17] and got[3].tolist() == [1, 2]
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (9, 2)])
+def test_replay_of_a_schedule(dev, window, sinks):
+    """An ISJL schedule played on the operators: every request's every token attends over
+    exactly the request's own tokens, whatever pages they went to.  The reference keeps
+    queries and keys in 64 bits; their rounding to f16 moves a score by at most
+    d = (2 u + u^2) scale sum |q k|, and the output by (exp(2 d) - 1) A beside its own
+    rounding."""
+    import numpy as np
+    import torch
+    from paper_2608_02244_amd import replay
+    rng = np.random.default_rng(5)
+    n, Hq, Hkv, D, page, layers, u = 12, 4, 2, 64, 4, 2, U["f16"]
+    a, p, o = (rng.integers(lo, hi, (1, n)).astype(np.int32)
+               for lo, hi in ((0, 20), (1, 20), (1, 30)))
+    _, start, finish = fs.simulate(a, p, o, policy="isjl", B=4, alpha=8, M_kv=160, cost_c=0,
+                                   cost_tau=0, schedule=True)
+    length = (p + o)[0].tolist()
+    g = torch.Generator().manual_seed(9)
+    x = torch.randn(layers, n, max(length), Hq + 2 * Hkv, D, generator=g).half()
+    xd = x.to(dev)
+    w = replay.Worker(n_pages=160 // page + n, page_size=page, q_heads=Hq, kv_heads=Hkv,
+                      head_dim=D, max_len=max(length), layers=layers, window=window,
+                      n_sink=sinks, dtype=torch.float16, device=dev)
+    pages = len(w.free)
+    got = torch.zeros(layers, n, max(length), Hq, D, dtype=torch.float64)
+    seen = [0] * n
+
+    def on_step(t, now, outs):
+        for i, r in enumerate(now):
+            for layer, y in enumerate(outs):
+                got[layer, r, seen[r]] = y[i].double().cpu()
+            seen[r] += 1
+    replay.play(w, start[0], finish[0],
+                lambda layer, now, at: torch.stack([xd[layer, r, i] for r, i in zip(now, at)]),
+                on_step)
+    assert seen == length
+    assert sorted(w.free.tolist()) == list(range(pages))  # every page came back, once
+    y = x.double()
+    y[..., :Hq + Hkv, :] /= (y[..., :Hq + Hkv, :].square().mean(-1, keepdim=True) + 1e-6).sqrt()
+    cs = w.cos_sin.double().cpu()[:max(length), None, :]
+    c, s = cs[..., :D // 2], cs[..., D // 2:]
+    f, e = y[..., :Hq + Hkv, :D // 2].clone(), y[..., :Hq + Hkv, D // 2:].clone()
+    y[..., :Hq + Hkv, :D // 2], y[..., :Hq + Hkv, D // 2:] = f * c - e * s, e * c + f * s
+    for layer in range(layers):
+        for r in range(n):
+            for h in range(Hq):
+                z = y[layer, r, :length[r]]
+                q, k, v = z[:, h], z[:, Hq + h // 2], z[:, Hq + Hkv + h // 2]
+                i = torch.arange(length[r])
+                hide = i[None, :] > i[:, None]
+                if window:
+                    hide |= (i[None, :] <= i[:, None] - window) & (i[None, :] >= sinks)
+                wt = torch.softmax((q @ k.t() * D ** -0.5).masked_fill(hide, -math.inf), 1)
+                ref, A = wt @ v, wt @ v.abs()
+                d = (2 * u + u * u) * D ** -0.5 * (q.abs() @ k.abs().t()).amax(1, keepdim=True)
+                tol = (torch.exp(2 * d) - 1) * A + 1.1 * u * (A + ref.abs()) + 2.0 ** -18 * (1 + A)
+                assert ((got[layer, r, :length[r], h] - ref).abs() <= tol).all()
