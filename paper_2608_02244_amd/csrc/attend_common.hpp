@@ -1,4 +1,4 @@
-// Parts shared by the attention kernels (attend_rows.hip, attend_tiles.hip,
+// Parts shared by the attention kernels (attend_rows.hpp, attend_tiles.hpp,
 // attend.hip).
 //
 // Every kernel keeps, per row (a token and query head), the running maximum m of
