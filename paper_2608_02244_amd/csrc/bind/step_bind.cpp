@@ -35,6 +35,8 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
 c10::DeviceGuard one_device(PyObject* const* a, Py_ssize_t n) {
   const at::Tensor* first = nullptr;
   for (Py_ssize_t i = 0; i < n; ++i) {
+    // numbers first: the tensor check is an isinstance() for them (0.2 us a call in all)
+    if (a[i] == Py_None || PyLong_Check(a[i]) || PyFloat_Check(a[i])) continue;
     if (!THPVariable_Check(a[i])) continue;
     const at::Tensor& t = THPVariable_Unpack(a[i]);
     if (!first) first = &t;
