@@ -51,7 +51,13 @@ struct RowsPlan {
 };
 
 constexpr int UNIT = 32;       // keys of a unit
-constexpr int MOST_PARTS = 32;  // of a tile, on average
+// Parts of a tile, on average.  More spread a lone long request over more waves, and cost
+// the join more.  One request, a call with 8 / 32 / 128 / 256 parts at most:
+//   131,072 tokens, 8 key heads   885 / 243 /  98 / 106 us (5.5 TB/s at 128)
+//    16,384 tokens, 8 key heads   114 /  44 /  27 /  36 us
+//    65,536 tokens, 1 key head    422 / 108 /  46 /  40 us
+//     4,096 tokens, 1 key head     31 /  17 /  18 /  18 us
+constexpr int MOST_PARTS = 128;
 
 // Blocks per compute unit that the registers allow.
 constexpr int rows_occupancy(int D) { return D == 64 ? 3 : 2; }

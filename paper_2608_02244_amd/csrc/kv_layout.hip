@@ -23,7 +23,9 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int MAX_REQ = FSCHED_MAX_REQ;
-constexpr int MAX_BLOCKS = 512;  // more would only repeat the sums
+// More would only repeat the sums (1,024 prompts, 1.4 M tokens: 31.4 us with 128 blocks,
+// 13.0 with 512, 13.5 with 1,024).
+constexpr int MAX_BLOCKS = 512;
 constexpr int TOK = 4;  // tokens per thread and turn: one 16-byte store each
 
 __device__ __forceinline__ int32_t sat32(int64_t x) {

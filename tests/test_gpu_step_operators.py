@@ -478,6 +478,13 @@ def test_attend_long_prompt(dev, dt):
     Batch(dev, [300], [900], 2, 2, 64, dt, page=4, window=70, sinks=3).check()
 
 
+@pytest.mark.parametrize("D,page,own", [(128, 16, [20000]), (64, 8, [9001, 1]),
+                                        (256, 64, [12000])])
+def test_attend_decode_one_long_request(dev, D, page, own):
+    """One request's keys spread over the device, in hundreds of parts."""
+    Batch(dev, [1] * len(own), own, 4, 1, D, page=page).check()
+
+
 @pytest.mark.parametrize("prefix", [1, 15, 16, 17, 100, 640])
 @pytest.mark.parametrize("mode", ["decode", "draft", "chunk"])
 def test_shared_prefix(dev, prefix, mode):
