@@ -28,6 +28,7 @@ class Worker:
                  window: int = 0, n_sink: int = 0, dtype=torch.bfloat16, device="cuda"):
         self.page_size, self.q_heads, self.window, self.n_sink = (page_size, q_heads, window,
                                                                   n_sink)
+        self.max_len = max_len  # rows of the rotation table; the block table's are whole pages
         self.width = -(-max_len // page_size)
         self.caches = [tuple(torch.zeros(n_pages, kv_heads, page_size, head_dim, dtype=dtype,
                                          device=device) for _ in range(2))
@@ -70,11 +71,11 @@ class Worker:
         the fused projection [sum(new), q_heads + 2 kv_heads, head_dim] of a layer.  Returns
         every layer's attention output."""
         old = [self.held[r] for r in self.requests]
+        if any(o + n > self.max_len for o, n in zip(old, new)):
+            raise ValueError("a request outgrows max_len")
         need = sum(self._pages(o + n) - self._pages(o) for o, n in zip(old, new))
         if need > len(self.free):
             raise RuntimeError(f"the step needs {need} pages, {len(self.free)} are free")
-        if any(o + n > self.width * self.page_size for o, n in zip(old, new)):
-            raise ValueError("a request outgrows max_len")
         dev = self.table.device
         lengths = torch.tensor([old, list(new)], dtype=torch.int32, device=dev)
         slots, pos, q_start, kv_len, _ = fs.kv_layout(

@@ -1,0 +1,67 @@
+"""What ``replay`` decides on the host, without a GPU: a worker on the CPU whose operators
+are plain stand-ins (places in a cache, no arithmetic)."""
+import pytest
+import torch
+
+import paper_2608_02244_amd as fs
+from paper_2608_02244_amd import replay
+
+
+@pytest.fixture
+def plain(monkeypatch):
+    """kv_layout as the operator does it, one token after the other; the queries go
+    through the other two unchanged."""
+    def kv_layout(old, new, table, free, *, page_size, n_tok):
+        slots, pos, start, taken = [], [], [0], 0
+        for r, (o, m) in enumerate(zip(old.tolist(), new.tolist())):
+            for c in range(-(-o // page_size), -(-(o + m) // page_size)):
+                table[r, c] = free[taken]
+                taken += 1
+            for i in range(o, o + m):
+                slots.append(int(table[r, i // page_size]) * page_size + i % page_size)
+                pos.append(i)
+            start.append(start[-1] + m)
+        assert start[-1] == n_tok
+        return tuple(torch.tensor(x, dtype=torch.int32)
+                     for x in (slots, pos, start, (old + new).tolist(), [taken, n_tok]))
+
+    def qk_norm_rope(qkv, *args, **kw):
+        return qkv[:, :2]
+
+    def attend(q, *args, **kw):
+        return q
+    for f in (kv_layout, qk_norm_rope, attend):
+        monkeypatch.setattr(fs, f.__name__, f, raising=False)
+
+
+def worker(**kw):
+    v = dict(n_pages=8, page_size=4, q_heads=2, kv_heads=1, head_dim=64, max_len=10, device="cpu")
+    v.update(kw)
+    return replay.Worker(**v)
+
+
+def projection(tokens):
+    return torch.zeros(tokens, 4, 64, dtype=torch.bfloat16)
+
+
+def pages(w):
+    """Ids of the free pages and of those that the requests hold."""
+    held = [int(x) for r, row in zip(w.requests, w.table)
+            for x in row[:-(-w.held[r] // w.page_size)]]
+    return sorted(w.free.tolist()), sorted(held)
+
+
+def test_a_request_stays_within_max_len(plain):
+    """10 tokens end inside the third page: the eleventh has a slot, but no row of the
+    rotation table."""
+    w = worker()
+    w.admit([7])
+    w.step([10], lambda layer: projection(10))
+    before = pages(w), dict(w.held), w.table.clone()
+    with pytest.raises(ValueError, match="max_len"):
+        w.step([1], lambda layer: projection(1))
+    assert (pages(w), w.held) == before[:2] and torch.equal(w.table, before[2])
+    w = worker()
+    w.admit([0])
+    with pytest.raises(ValueError, match="max_len"):
+        w.step([11], lambda layer: projection(11))
