@@ -81,13 +81,14 @@ class Worker:
         slots, pos, q_start, kv_len, _ = fs.kv_layout(
             lengths[0], lengths[1], self.table, self.free, page_size=self.page_size,
             n_tok=sum(new))
-        self.free = self.free[need:]
         out = []
         for layer, (k, v) in enumerate(self.caches):
             q = fs.qk_norm_rope(qkv(layer), pos, slots, self.cos_sin, k, v, self.weight,
                                 self.weight)
             out.append(fs.attend(q, k, v, self.table, q_start, kv_len, window=self.window,
                                  n_sink=self.n_sink, max_q=max([1, *new])))
+        # only now: a step that ends with an error (in ``qkv``, say) can be run again
+        self.free = self.free[need:]
         for r, o, n in zip(self.requests, old, new):
             self.held[r] = o + n
         return out

@@ -65,3 +65,24 @@ def test_a_request_stays_within_max_len(plain):
     w.admit([0])
     with pytest.raises(ValueError, match="max_len"):
         w.step([11], lambda layer: projection(11))
+
+
+def test_a_step_that_fails_can_be_run_again(plain):
+    """An error between the placement and the last layer loses no page."""
+    w = worker(layers=2)
+    w.admit([0, 1])
+    w.step([3, 1], lambda layer: projection(4))
+
+    def broken(layer):
+        if layer == 1:
+            raise RuntimeError("no projection")
+        return projection(6)
+    before = pages(w)
+    with pytest.raises(RuntimeError, match="no projection"):
+        w.step([2, 4], broken)
+    assert pages(w) == before and w.held == {0: 3, 1: 1}
+    w.step([2, 4], lambda layer: projection(6))
+    free, held = pages(w)
+    assert len(held) == 4 and sorted(free + held) == list(range(8))
+    w.release([0, 1])
+    assert pages(w) == (list(range(8)), [])
