@@ -49,6 +49,8 @@ class Worker:
     def release(self, ids) -> None:
         """Finished requests give their pages back."""
         gone = set(ids)
+        if not gone <= self.held.keys():
+            raise ValueError(f"not among the requests: {sorted(gone - self.held.keys())}")
         back = [self.table[i, :self._pages(self.held[r])]
                 for i, r in enumerate(self.requests) if r in gone]
         keep = [i for i, r in enumerate(self.requests) if r not in gone]
@@ -61,6 +63,8 @@ class Worker:
     def admit(self, ids) -> None:
         """Requests that hold nothing yet get a row."""
         ids = list(ids)
+        if len({*self.requests, *ids}) < len(self.requests) + len(ids):
+            raise ValueError("a request has one row only")
         fresh = self.table.new_full((len(ids), self.width), -1)
         self.table = torch.cat((self.table, fresh))
         self.requests += ids

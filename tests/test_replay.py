@@ -86,3 +86,17 @@ def test_a_step_that_fails_can_be_run_again(plain):
     assert len(held) == 4 and sorted(free + held) == list(range(8))
     w.release([0, 1])
     assert pages(w) == (list(range(8)), [])
+
+
+def test_release_and_admit_refuse_ids_before_they_change_anything(plain):
+    w = worker()
+    w.admit([3, 5])
+    w.step([5, 2], lambda layer: projection(7))
+    before = pages(w), list(w.requests), dict(w.held), w.table.clone()
+    for call in (lambda: w.release([3, 4]), lambda: w.admit([6, 5]), lambda: w.admit([6, 6])):
+        with pytest.raises(ValueError):
+            call()
+        assert (pages(w), w.requests, w.held) == before[:3] and torch.equal(w.table, before[3])
+    w.release([5])
+    w.admit([5])
+    assert w.held == {3: 5, 5: 0} and w.requests == [3, 5]
