@@ -51,6 +51,8 @@ class Worker:
         gone = set(ids)
         if not gone <= self.held.keys():
             raise ValueError(f"not among the requests: {sorted(gone - self.held.keys())}")
+        if not gone:
+            return
         back = [self.table[i, :self._pages(self.held[r])]
                 for i, r in enumerate(self.requests) if r in gone]
         keep = [i for i, r in enumerate(self.requests) if r not in gone]
@@ -63,6 +65,8 @@ class Worker:
     def admit(self, ids) -> None:
         """Requests that hold nothing yet get a row."""
         ids = list(ids)
+        if not ids:
+            return
         if len({*self.requests, *ids}) < len(self.requests) + len(ids):
             raise ValueError("a request has one row only")
         fresh = self.table.new_full((len(ids), self.width), -1)

@@ -100,3 +100,15 @@ def test_release_and_admit_refuse_ids_before_they_change_anything(plain):
     w.release([5])
     w.admit([5])
     assert w.held == {3: 5, 5: 0} and w.requests == [3, 5]
+
+
+def test_release_and_admit_of_nobody_leave_the_table_alone(plain):
+    """No copy of the table and no index from the host at the steps (nearly all of a
+    schedule's) at which no request starts or finishes."""
+    w = worker()
+    w.admit([0])
+    w.step([5], lambda layer: projection(5))
+    table, free = w.table, w.free
+    w.release([])
+    w.admit([])
+    assert w.table is table and w.free is free
