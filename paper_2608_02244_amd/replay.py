@@ -102,13 +102,23 @@ class Worker:
         return out
 
 
-def play(worker: Worker, start, finish, qkv: Callable, on_step: Callable = None) -> int:
+def play(worker: Worker, start, finish, qkv: Callable, on_step: Callable = None, *,
+         lengths=None) -> int:
     """Runs a schedule of one instance (``start`` and ``finish`` as ``simulate`` returns
-    them: a request's first step, and the step after its last) and returns the number of steps with tokens.
+    them: a request's first step, and the step after its last) and returns the number of
+    steps with tokens.
 
     ``qkv(layer, requests, positions)`` gives a step's projection (one token per request
-    at its position); ``on_step(step, requests, outputs)`` sees what came out."""
+    at its position); ``on_step(step, requests, outputs)`` sees what came out.
+    ``lengths``: prompt + output tokens of every request.  With them a schedule in which
+    some request runs another number of steps is refused: one made with ``prefill=True``,
+    whose prompts take no steps of their own, is not what this plays."""
     start, finish = [int(x) for x in start], [int(x) for x in finish]
+    if lengths is not None:
+        lengths = [int(x) for x in lengths]
+        if [f - s for s, f in zip(start, finish)] != lengths:
+            raise ValueError("the schedule's requests do not run one step per token (was it "
+                             "made with prefill=True?)")
     steps = 0
     for t in range(min(start, default=0), max(finish, default=0)):
         worker.release([r for r in worker.requests if finish[r] <= t])

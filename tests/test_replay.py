@@ -112,3 +112,15 @@ def test_release_and_admit_of_nobody_leave_the_table_alone(plain):
     w.release([])
     w.admit([])
     assert w.table is table and w.free is free
+
+
+def test_play_refuses_a_schedule_whose_steps_are_not_the_tokens(plain):
+    """Two requests of 3 + 2 and 1 + 4 tokens: prefilled they run 2 and 4 steps."""
+    w, tokens = worker(), []
+    with pytest.raises(ValueError, match="prefill"):
+        replay.play(w, [0, 1], [2, 5], lambda layer, now, at: projection(len(now)),
+                    lengths=[5, 5])
+    assert not w.requests
+    assert replay.play(w, [0, 1], [5, 6], lambda layer, now, at: projection(len(now)),
+                       lambda t, now, out: tokens.append(len(out[0])), lengths=[5, 5]) == 6
+    assert sum(tokens) == 10 and pages(w) == (list(range(8)), [])
