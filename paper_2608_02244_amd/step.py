@@ -9,7 +9,8 @@ flows through them.
 
 With ``stream`` (a torch.cuda.Stream) a call runs as under ``torch.cuda.stream``: its
 outputs and workspace are allocated for that stream, and the caller orders the
-streams (inputs written on another one; results read on another one).
+streams (inputs written on another one; results read on another one).  It is a stream of
+the tensors' device (ValueError).
 
 A cache is a pair of tensors [n_pages, kv_heads, page_size, head_dim]; a permuted
 view (another order of page, head and slot in memory) does as well, as long as the
@@ -64,6 +65,14 @@ def _current(x):
     return torch._C._cuda_getCurrentRawStream(x.get_device()) if x.is_cuda else 0
 
 
+def _on(stream, x):
+    """``stream`` as torch's current one; it must be of the device of ``x``, whose current
+    stream a call takes."""
+    if isinstance(x, torch.Tensor) and x.device != stream.device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors are on {x.device}")
+    return torch.cuda.stream(stream)
+
+
 def kv_layout(old_len, new_len, block_table, free_pages, *, page_size: int, n_tok: int,
               first_pos: int = 0, stream=None):
     """fsched_kv_layout: places for the step's new tokens.
@@ -71,7 +80,7 @@ def kv_layout(old_len, new_len, block_table, free_pages, *, page_size: int, n_to
     ``block_table`` [n_req, width] is updated in place.  Returns (slots [n_tok],
     positions [n_tok], q_start [n_req + 1], kv_len [n_req], used [2]), int32."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, old_len):
             return kv_layout(old_len, new_len, block_table, free_pages, page_size=page_size,
                              n_tok=n_tok, first_pos=first_pos)
     return _step.kv_layout(old_len, new_len, block_table, free_pages, page_size, n_tok, first_pos,
@@ -85,7 +94,7 @@ def qk_norm_rope(qkv, positions, slots, cos_sin, k_cache, v_cache, q_weight=None
     values put into the caches at ``slots`` (None: nowhere).  ``cos_sin`` [n_pos,
     rot_dim] f32 (None: no rotation, ``positions`` may be None)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, qkv):
             return qk_norm_rope(qkv, positions, slots, cos_sin, k_cache, v_cache, q_weight,
                                 k_weight, eps=eps, interleaved=interleaved, out=out)
     return _step.qk_norm_rope(qkv, positions, slots, cos_sin, k_cache, v_cache, q_weight,
@@ -106,7 +115,7 @@ def attend(q, k_cache, v_cache, block_table, q_start, kv_len, *, scale=None, win
     torch's allocator.
     Returns out, or (out, lse [n_tok, q_heads] float32) with ``return_lse``."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, q):
             return attend(q, k_cache, v_cache, block_table, q_start, kv_len,
                           scale=scale, window=window, n_sink=n_sink, max_q=max_q, out=out,
                           return_lse=return_lse, workspace=workspace)
@@ -121,7 +130,7 @@ def attend_shared(q, k_cache, v_cache, prefix_pages, prefix_len: int, block_tabl
     ``prefix_len`` tokens held in ``prefix_pages``; ``block_table`` and ``kv_len``
     describe each request's own tokens behind them."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, q):
             return attend_shared(q, k_cache, v_cache, prefix_pages, prefix_len, block_table,
                                  q_start, kv_len, scale=scale, window=window, n_sink=n_sink,
                                  max_q=max_q, out=out, return_lse=return_lse,
