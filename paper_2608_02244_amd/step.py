@@ -61,8 +61,11 @@ class AttnParams(ctypes.Structure):
 
 
 def _current(x):
-    """Address of torch's current stream."""
-    return torch._C._cuda_getCurrentRawStream(x.get_device()) if x.is_cuda else 0
+    """Address of torch's current stream on the device of ``x`` (what is no GPU tensor the
+    call itself refuses)."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        return 0
+    return torch._C._cuda_getCurrentRawStream(x.get_device())
 
 
 def _on(stream, x):

@@ -25,3 +25,10 @@ def test_a_stream_of_another_device_is_refused():
     for call in calls(torch.zeros(4, dtype=torch.int32), stream=other):
         with pytest.raises(ValueError, match="stream is on cuda:1"):
             call()
+
+
+def test_a_first_argument_that_is_no_tensor_is_refused_like_the_others():
+    for first in ([0, 0, 0, 0], None, 7):
+        for call in calls(first):
+            with pytest.raises(ValueError, match="must be a"):
+                call()
