@@ -303,7 +303,10 @@ _STEP = ("attend", "attend_shared", "attend_workspace", "kv_layout", "qk_norm_ro
 def __getattr__(name):
     """The step operators (module ``step``), loaded with torch on their first use."""
     if name in _STEP:
-        from . import step
+        try:
+            from . import step
+        except RuntimeError as e:  # the binding is not built: hasattr() may say so
+            raise AttributeError(f"{name}: {e}") from e
         globals().update((n, getattr(step, n)) for n in _STEP)
         return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

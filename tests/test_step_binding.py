@@ -1,5 +1,9 @@
 """What the binding of the step operators refuses before it calls the library, without a
 GPU."""
+import os
+import shutil
+import subprocess
+import sys
 import types
 
 import pytest
@@ -32,3 +36,23 @@ def test_a_first_argument_that_is_no_tensor_is_refused_like_the_others():
         for call in calls(first):
             with pytest.raises(ValueError, match="must be a"):
                 call()
+
+
+def test_without_the_binding_the_package_says_so_and_hasattr_answers(tmp_path):
+    """A copy of the package without _step.so: the evaluation calls are there, the step
+    operators are missing attributes whose message names the cause."""
+    copy = tmp_path / "paper_2608_02244_amd"
+    copy.mkdir()
+    for name in ("__init__.py", "step.py"):
+        shutil.copy(os.path.join(os.path.dirname(fs.__file__), name), copy)
+    code = ("import paper_2608_02244_amd as fs\n"
+            "assert fs.__file__.startswith(%r), fs.__file__\n"
+            "assert hasattr(fs, 'simulate') and not hasattr(fs, 'attend')\n"
+            "try: fs.kv_layout\n"
+            "except AttributeError as e: assert '_step.so is not built' in str(e), e\n"
+            "else: raise AssertionError\n"
+            "try: from paper_2608_02244_amd import step\n"
+            "except RuntimeError as e: assert '_step.so is not built' in str(e), e\n"
+            "else: raise AssertionError\n" % str(tmp_path))
+    r = subprocess.run([sys.executable, "-c", code], cwd=tmp_path, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
