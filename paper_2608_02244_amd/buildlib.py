@@ -2,13 +2,15 @@
 
 Every HIP translation unit under csrc/ is compiled in parallel, then linked
 into one shared library next to this file; the binding of the step's operators
-(csrc/bind) becomes an extension module beside it, compiled against torch.  No CPU
-fallback is built.
+(csrc/bind) becomes an extension module beside it, compiled against torch (left out
+where torch is not installed: the evaluation calls work on numpy arrays without it).
+No CPU fallback is built.
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
 import glob
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -65,6 +67,12 @@ def _run(cmd: list, what: str) -> None:
         raise RuntimeError(f"{what} failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
 
 
+def _cxx() -> list:
+    """A host C++ compiler: hipcc where there is no other."""
+    found = shutil.which("g++") or shutil.which("c++")
+    return [found] if found else [_hipcc()]
+
+
 def _compile_bind() -> str:
     """Object file of the binding (host code only)."""
     import sysconfig
@@ -72,11 +80,10 @@ def _compile_bind() -> str:
     import torch
     from torch.utils import cpp_extension
     obj = os.path.join(BUILD_DIR, "step_bind.o")
-    cxx = shutil.which("g++") or "c++"
     inc = cpp_extension.include_paths() + [sysconfig.get_paths()["include"], INCLUDE]
-    _run([cxx, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
-          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
-         [f"-I{p}" for p in inc] + ["-c", BIND_SRC, "-o", obj], "compile")
+    _run(_cxx() + ["-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
+                   f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"] +
+         [f"-I{p}" for p in inc] + ["-x", "c++", "-c", BIND_SRC, "-o", obj], "compile")
     return obj
 
 
@@ -84,10 +91,9 @@ def _link_bind(obj: str) -> None:
     """The extension module, which finds libfsched.so beside it (torch's libraries are
     loaded by the time it is imported)."""
     from torch.utils import cpp_extension
-    cxx = shutil.which("g++") or "c++"
     lib = cpp_extension.library_paths()[0]
     tmp = BIND_LIB + ".tmp"
-    _run([cxx, "-shared", "-o", tmp, obj, f"-L{HERE}", "-lfsched", f"-L{lib}", "-lc10",
+    _run(_cxx() + ["-shared", "-o", tmp, obj, f"-L{HERE}", "-lfsched", f"-L{lib}", "-lc10",
           "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN"], "link")
     os.replace(tmp, BIND_LIB)
 
@@ -96,15 +102,21 @@ def build(jobs: int | None = None, verbose: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.cpp")))
     jobs = jobs or min(len(srcs), os.cpu_count() or 4, 16)
+    with_bind = importlib.util.find_spec("torch") is not None
     with cf.ThreadPoolExecutor(max_workers=jobs) as ex:
-        bind = ex.submit(_compile_bind)
+        bind = ex.submit(_compile_bind) if with_bind else None
         objs = list(ex.map(_compile, srcs))
-        bind_obj = bind.result()
+        bind_obj = bind.result() if with_bind else None
     tmp = LIB + ".tmp"
     cmd = [_hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + objs
     _run(cmd, "link")
     os.replace(tmp, LIB)
-    _link_bind(bind_obj)
+    if with_bind:
+        _link_bind(bind_obj)
+    else:
+        if os.path.exists(BIND_LIB):
+            os.remove(BIND_LIB)  # of an older libfsched.so
+        print("torch is not installed: built without the step operators' binding")
     if verbose:
         print(f"built {LIB}")
     return LIB
