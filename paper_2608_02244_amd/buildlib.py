@@ -28,6 +28,7 @@ BUILD_DIR = os.path.join(HERE, "_build")
 ARCH = "gfx950"
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+          "-Werror=inline-asm",  # clobbers that the compiler does not honour
           f"-I{INCLUDE}", f"-I{CSRC}"]
 # Instruction scheduling strategies, chosen by measurement: the simulation
 # kernels (csrc/sim_*.hip) by LLVM's iterative max-occupancy strategy, the

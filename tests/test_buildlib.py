@@ -1,6 +1,7 @@
 """The build of the native libraries: what it needs, and what the compiler may not warn
 about (the compilers themselves run in ``__graft_entry__.build()``)."""
 import os
+import subprocess
 import sys
 
 import pytest
@@ -46,3 +47,25 @@ def test_binding_is_built_without_a_host_compiler(dry, monkeypatch):
     buildlib.build()
     bind = [c for c in dry if buildlib.BIND_SRC in c or buildlib.BIND_LIB + ".tmp" in c]
     assert len(bind) == 2 and all(c[0] == buildlib._hipcc() for c in bind)
+
+
+def test_direct_loads_to_lds_keep_the_compiler_s_registers(tmp_path):
+    """The loads take their LDS address from m0, a reserved register: naming it as
+    clobbered is not honoured (the compiler warns), so they have to put it back."""
+    src = tmp_path / "loads.hip"
+    src.write_text('''#include "attend_tiles.hpp"
+__global__ void two_loads(const char* p, unsigned off, unsigned base) {
+  fs::load_to_lds(p + threadIdx.x * 16, base);
+  fs::load_to_lds(p, off + threadIdx.x * 16, base + 1024);
+  fs::wait_loads();
+}
+''')
+    out = tmp_path / "loads.s"
+    r = subprocess.run([buildlib._hipcc(), *buildlib.COMMON, "-Werror=inline-asm", "-x", "hip",
+                        "--cuda-device-only", "-S", str(src), "-o", str(out)],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    writes = [x.split() for x in out.read_text().splitlines() if "s_mov_b32" in x and "m0" in x]
+    saved = [x[1].strip(",") for x in writes if x[2] == "m0"]
+    put_back = [x[2] for x in writes if x[1] == "m0,"]
+    assert len(saved) == 2 and put_back[1::2] == saved
