@@ -6,6 +6,7 @@
 
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -162,12 +163,8 @@ PyObject* guarded(Py_ssize_t got, Py_ssize_t want, F body) {
   } catch (const Raised&) {
   } catch (const Refused& e) {
     PyErr_SetString(PyExc_ValueError, e.what.c_str());
-  } catch (const c10::Error& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-  } catch (...) {
-    PyErr_SetString(PyExc_RuntimeError, "unknown C++ exception");
+  } catch (...) {  // torch's errors as torch raises them (torch.OutOfMemoryError, ...)
+    torch::translate_exception_to_python(std::current_exception());
   }
   return nullptr;
 }
