@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/MemoryOverlap.h>
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -106,6 +107,12 @@ const at::Tensor& rows(PyObject* o, int64_t dim, at::ScalarType type, const char
     throw Refused{std::string(name) + " must be a " + std::to_string(dim) + "-dimensional " +
                   dtype_name(type) + " GPU tensor whose last dimension is contiguous"};
   return t;
+}
+
+// What a call writes: no two of its elements may be one.
+void written(const at::Tensor& t, const char* name) {
+  if (at::has_internal_overlap(t) == at::MemOverlap::Yes)
+    throw Refused{std::string(name) + " is written and must not be an expanded tensor"};
 }
 
 struct Cache {
@@ -221,6 +228,10 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return guarded(n_args, 12, [&]() -> PyObject* {
     const c10::DeviceGuard on = one_device(a, n_args);
     const Cache c = cache(a[4], a[5]);
+    if (a[2] != Py_None) {  // slots
+      written(tensor(a[4], "k_cache"), "k_cache");
+      written(tensor(a[5], "v_cache"), "v_cache");
+    }
     const int64_t dim = c.c.head_dim;
     const at::Tensor& qkv = rows(a[0], 3, c.type, "qkv");
     const int64_t n = qkv.size(0), heads = qkv.size(1) - 2 * (int64_t)c.c.kv_heads;
@@ -250,6 +261,7 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                                             : rows(a[10], 3, c.type, "out");
     if (out.size(0) != n || out.size(1) != heads || out.size(2) != dim)
       throw Refused{"out must have shape [n_tok, q_heads, head_dim]"};
+    written(out, "out");
     p.n_tok = extent(n, "qkv");
     p.q_heads = extent(heads, "qkv");
     p.interleaved = truth(a[9]);
@@ -308,6 +320,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const at::Tensor out =
         a[12] == Py_None ? at::empty(q.sizes(), like(q, c.type)) : rows(a[12], 3, c.type, "out");
     if (out.sizes() != q.sizes()) throw Refused{"out and q differ in shape"};
+    written(out, "out");
     p.q_token_stride = q.stride(0);
     p.q_head_stride = q.stride(1);
     p.out_token_stride = out.stride(0);
