@@ -331,9 +331,13 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       workspace = tensor(a[14], "workspace");
       if (!workspace.is_cuda() || !workspace.is_contiguous())
         throw Refused{"workspace must be a contiguous GPU tensor"};
-    } else {
+    }
+    if (!workspace.defined() || workspace.nbytes() == 0) {
       int64_t need = 0;
       check(fsched_attend_workspace(&p, &c.c, &need), name);
+      // an empty tensor's address is that of no workspace, which the library would take
+      // from its pool
+      if (workspace.defined() && need > 0) check(FSCHED_ESCRATCH, name);
       if (need > 0) workspace = at::empty({need}, like(q, at::kByte));
     }
     void* stream = handle(a[15]);

@@ -45,3 +45,18 @@ def test_expanded_tensors_are_read_but_not_written(dev):
     got = fs.attend(same, k, *b.args[2:], scale=b.scale, max_q=2)
     want = fs.attend(same.contiguous(), k.contiguous(), *b.args[2:], scale=b.scale, max_q=2)
     assert torch.equal(got, want)
+
+
+def test_workspace_that_is_too_small_is_refused(dev):
+    import torch
+    b = Batch(dev, [1] * 20 + [50, 1], [37 * i % 900 + 1 for i in range(20)] + [800, 3], 16, 2, 128)
+    ws = fs.attend_workspace(len(b.q), len(b.own), 16, 2, 128, page_size=16,
+                             table_width=b.table.shape[1], max_q=50)
+    assert ws.numel() > 256
+    for room in (ws[:256], ws[:-1].clone(), torch.empty(0, dtype=torch.uint8, device=dev)):
+        with pytest.raises(fs.FschedError) as e:
+            b.call(workspace=room)
+        assert e.value.code == fs.ESCRATCH
+    out, _ = b.call()
+    got, _ = b.call(workspace=ws)
+    assert torch.equal(out, got)
