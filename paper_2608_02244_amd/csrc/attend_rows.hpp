@@ -59,8 +59,17 @@ constexpr int UNIT = 32;       // keys of a unit
 //     4,096 tokens, 1 key head     31 /  17 /  18 /  18 us
 constexpr int MOST_PARTS = 128;
 
-// Blocks per compute unit that the registers allow.
-constexpr int rows_occupancy(int D) { return D == 64 ? 3 : 2; }
+// Blocks per compute unit.  Fewer waves have longer pieces, more of them more loads under
+// way.  The registers would allow 4 with heads of 64 and 3 with heads of 128 (one row tile,
+// pages of 16 and more); two with heads of 256 would spill to scratch.  Calls in bf16 with
+// 1 / 2 / 3 / 4 blocks, us:
+//   heads of 128   512 requests, 0.73 M tokens, 4 key heads   262 / 251 / 275
+//                  64 requests, 65,000 tokens, 8 key heads     57 /  56 /  58
+//   heads of  64   400 requests, 0.57 M tokens, 8 key heads     - / 202 / 205 / 205
+//                  64 requests                                  - /  35 /  35 /  36
+//   heads of 256   64 requests, pages of 16 and of 8          108 / 117, 107 / 126
+//                  64 drafts; one request of 131,072 tokens   122 / 136, 218 / 211
+constexpr int rows_occupancy(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
 
 // WIDE: pages of 16 tokens and more, so that keys 0..15 and 16..31 of a unit lie in
 // one page each and their addresses are uniform but for a lane's constant offset.

@@ -1,6 +1,7 @@
 """The build of the native libraries: what it needs, and what the compiler may not warn
 about (the compilers themselves run in ``__graft_entry__.build()``)."""
 import os
+import re
 import subprocess
 import sys
 
@@ -69,3 +70,19 @@ __global__ void two_loads(const char* p, unsigned off, unsigned base) {
     saved = [x[1].strip(",") for x in writes if x[2] == "m0"]
     put_back = [x[2] for x in writes if x[1] == "m0,"]
     assert len(saved) == 2 and put_back[1::2] == saved
+
+
+@pytest.mark.parametrize("wide", ["true", "false"])
+def test_decode_kernels_of_heads_of_256_keep_their_registers(tmp_path, wide):
+    """Bound by the cache's bytes, they have none to spare for scratch."""
+    src = tmp_path / "rows.hip"
+    src.write_text(f'''#include "attend_main.hpp"
+template __global__ void fs::attend_rows_kernel<fs::Bf16, 256, 1, {wide}>(fs::AttnArgs, fs::MainPlan);
+template __global__ void fs::attend_rows_kernel<fs::F16, 256, 1, {wide}>(fs::AttnArgs, fs::MainPlan);
+''')
+    r = subprocess.run([buildlib._hipcc(), *buildlib.COMMON, "-Rpass-analysis=kernel-resource-usage",
+                        "-x", "hip", "--cuda-device-only", "-c", str(src), "-o",
+                        str(tmp_path / "rows.o")], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    scratch = re.findall(r"ScratchSize \[bytes/lane\]: (\d+)", r.stderr)
+    assert scratch == ["0", "0"]
