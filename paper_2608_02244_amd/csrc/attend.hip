@@ -250,7 +250,7 @@ void join(const AttnArgs& a, const JoinArgs& j, int head_dim, dim3 grid, hipStre
 
 }  // namespace
 
-size_t attend_workspace(const AttnArgs& a, int, int head_dim, int n_cu) {
+size_t attend_workspace(const AttnArgs& a, int head_dim, int n_cu) {
   return plan(a, head_dim, n_cu, nullptr).bytes;
 }
 

@@ -137,7 +137,7 @@ int attend_entry(const fsched_attn_params* p, const fsched_kv_cache* kv, const v
   a.lse = lse;
   hipStream_t s = (hipStream_t)stream;
   const int n_cu = fs::compute_units();
-  const size_t need = fs::attend_workspace(a, kv->dtype, kv->head_dim, n_cu);
+  const size_t need = fs::attend_workspace(a, kv->head_dim, n_cu);
   void* mine = nullptr;
   if (workspace) {
     if (((uintptr_t)workspace & 255) != 0) return FSCHED_EINVAL;
@@ -242,8 +242,7 @@ int fsched_attend_workspace(const fsched_attn_params* p, const fsched_kv_cache* 
   if (rc) return rc;
   *bytes = 0;
   if (p->n_tok == 0 || p->n_req == 0) return FSCHED_OK;
-  *bytes = (int64_t)fs::attend_workspace(attn_args(p, kv), kv->dtype, kv->head_dim,
-                                         fs::compute_units());
+  *bytes = (int64_t)fs::attend_workspace(attn_args(p, kv), kv->head_dim, fs::compute_units());
   return FSCHED_OK;
 }
 

@@ -60,7 +60,7 @@ hipError_t launch_kv_layout(const LayoutArgs& a, hipStream_t s);
 hipError_t launch_qk_rope(const RopeArgs& a, int dtype, int head_dim, int n_cu, hipStream_t s);
 
 // Workspace bytes of one attention call on a device of n_cu compute units.
-size_t attend_workspace(const AttnArgs& a, int dtype, int head_dim, int n_cu);
+size_t attend_workspace(const AttnArgs& a, int head_dim, int n_cu);
 hipError_t launch_attend(const AttnArgs& a, int dtype, int head_dim, int n_cu, void* workspace,
                          hipStream_t s);
 
