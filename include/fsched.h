@@ -301,9 +301,10 @@ int fsched_simulate_noalloc(const fsched_params* p, int64_t n_inst, int32_t n_jo
  *     page id outside 0 .. n_pages-1 holds no keys (what sits there is masked);
  *     a slot outside the cache is not written.
  *   - Elements are bf16 or f16; products accumulate and norms, softmax
- *     statistics and rotations run in 32 bits.  Strides are in elements.  The
- *     head dimension is contiguous; every other stride is a multiple of 8 and
- *     every base pointer 16-byte aligned (EINVAL otherwise).
+ *     statistics and rotations run in 32 bits.  The softmax weights are rounded
+ *     to the elements' type for their product with the values.  Strides are in
+ *     elements.  The head dimension is contiguous; every other stride is a
+ *     multiple of 8 and every base pointer 16-byte aligned (EINVAL otherwise).
  *   - At most FSCHED_MAX_REQ requests and FSCHED_MAX_STEP_TOKENS new tokens in a
  *     step (ETOOLARGE).  Sizes of zero are valid and do nothing. */
 #define FSCHED_MAX_REQ 4096
@@ -450,9 +451,10 @@ int fsched_qk_norm_rope(const fsched_rope_params* p, const fsched_kv_cache* kv, 
  *
  * fsched_attend_shared — the same for requests that all begin with one prefix of
  * prefix_len tokens, whose keys and values are held once, in prefix_pages
- * [ceil(prefix_len / page_size)], and read once for all requests.  kv_len and the
- * block table describe each request's own tokens, which follow the prefix: token i
- * sits at prefix_len + kv_len[r] - q_r + i. */
+ * [ceil(prefix_len / page_size)], and read once for every 128 rows of a key head
+ * (tokens times the query heads that read it) rather than for every request.
+ * kv_len and the block table describe each request's own tokens, which follow the
+ * prefix: token i sits at prefix_len + kv_len[r] - q_r + i. */
 typedef struct {
   int32_t n_req, n_tok, q_heads, max_q, table_width, window, n_sink, prefix_len;
   float scale;

@@ -5,6 +5,13 @@
 // its scores in base 2, the sum l of 2^(s - m) and the unnormalised output o.
 // Parts over disjoint keys join by  m = max m_i,  l = sum l_i 2^(m_i - m),
 // o = sum o_i 2^(m_i - m);  the result is o / l and lse = (m + log2 l) ln 2.
+//
+// Scores, m, l and o are 32-bit.  The weights 2^(s - m) are rounded to the values' type for
+// the second product, whose operands the matrix unit takes in 16 bits; l sums them before
+// that, so lse keeps its 32 bits.  Relative distance of the outputs from 64 bits: 2.2e-3 in
+// bf16 and 2.7e-4 in f16, against 1.7e-3 and 2.1e-4 where only the result is rounded.  A
+// second product with the weights' remainders would take that back for half as many
+// products again.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -14,7 +21,10 @@
 namespace fs {
 
 constexpr int ATT_THREADS = 256, ATT_WAVES = ATT_THREADS / 64;
-constexpr int WIDE_SHIFT = 4;  // the kernels' WIDE forms are for pages of 2^4 tokens and more
+// The kernels' WIDE forms are for pages of 2^4 tokens and more.  With and without them:
+// prompts 672 / 718 us a call, chunks beside decoding requests 109 / 111; decode alike (64
+// requests 55.6 / 55.1).
+constexpr int WIDE_SHIFT = 4;
 constexpr float NEG_INF = -__builtin_inff();
 constexpr float LN2 = 0.6931471805599453f;
 

@@ -52,11 +52,11 @@ struct RowsPlan {
 
 constexpr int UNIT = 32;       // keys of a unit
 // Parts of a tile, on average.  More spread a lone long request over more waves, and cost
-// the join more.  One request, a call with 8 / 32 / 128 / 256 parts at most:
-//   131,072 tokens, 8 key heads   885 / 243 /  98 / 106 us (5.5 TB/s at 128)
-//    16,384 tokens, 8 key heads   114 /  44 /  27 /  36 us
-//    65,536 tokens, 1 key head    422 / 108 /  46 /  40 us
-//     4,096 tokens, 1 key head     31 /  17 /  18 /  18 us
+// the join more.  One request, heads of 128, a call with 8 / 32 / 128 / 256 parts at most:
+//   131,072 tokens, 8 key heads   890 / 245 /  97 / 106 us (5.5 TB/s at 128)
+//    16,384 tokens, 8 key heads   120 /  45 /  27 /  36 us
+//    65,536 tokens, 1 key head    436 / 119 /  49 /  42 us
+//     4,096 tokens, 1 key head     35 /  17 /  18 /  18 us
 constexpr int MOST_PARTS = 128;
 
 // Blocks per compute unit.  Fewer waves have longer pieces, more of them more loads under
@@ -318,7 +318,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const RowsPlan& p
         for (int j = 0; j < 8; ++j) {
           e[j] = exp2_fast(fmaf(s[j >> 2][j & 3], a.scale_log2, -base));
           l[t] += e[j];
-          p[t][j] = (elem)e[j];  // rounded to the type of the values, as the products need
+          p[t][j] = (elem)e[j];  // the second product's operand (attend_common.hpp)
         }
       }
 

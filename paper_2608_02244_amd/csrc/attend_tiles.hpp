@@ -14,10 +14,12 @@
 // of 32 keys at once, the second 64 bytes of 8 keys.
 //
 // Bound by the products.  Measured (heads of 128, bf16): prompts of 25,600 tokens in all,
-// 680 us a call or 880 TFLOP/s.  Reading the operands one step ahead of their products,
+// 667 to 728 us a call (898 to 823 TFLOP/s) on the cards that it ran on, once some 25 calls
+// have gone before; the first ten take 750 to 850, while the clock finds its level.  As
+// launches among such first ones: reading the operands one step ahead of their products,
 // uniform load addresses and clearing absent keys in LDS rather than in each operand took
-// that call from 985 to 800 us (traced), masks without branches and lane-computed
-// addresses from 790 to 757 us.
+// them from 985 to 800 us, masks without branches and lane-computed addresses from 790 to
+// 757 us.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -468,7 +470,7 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
       for (int i = 0; i < 8; ++i) {
         const float e = exp2_fast(fmaf(s[g / 2][8 * (g & 1) + i], a.scale_log2, -base));
         l += e;
-        p[g & 1][i] = (elem)e;  // rounded to the type of the values, as the products need
+        p[g & 1][i] = (elem)e;  // the second product's operand (attend_common.hpp)
       }
     };
     weights(0);
