@@ -476,6 +476,143 @@ int fsched_attend_shared(const fsched_attn_params* p, const fsched_kv_cache* kv,
 int fsched_attend_workspace(const fsched_attn_params* p, const fsched_kv_cache* kv,
                             int64_t* bytes);
 
+/* ------------------------------------------------------------------------
+ * A cache within a budget: 4 bits an element hold more tokens in the same bytes,
+ * and pages whose tokens nobody looks at any more are given up.  The conventions
+ * are those of the step's operators above.
+ *
+ * A cache of 4 bits.  32 neighbouring elements x of a head share a scale s = 2^e,
+ * the least with max |x| <= 6 s, and each is held as the nearest of
+ * +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} s (of two equally near the one whose code is even).
+ * Codes are the values' places in that list, 8 added for a negative one; byte i of a
+ * token's codes holds elements 2i (low) and 2i + 1; a scale is the byte e + 127, or 255
+ * where the 32 elements are not all finite (they then stand for NaN).  e is -125 .. 125
+ * in bf16 and -23 .. 13 in f16 (magnitudes above 49,152 are held as that), so that every
+ * held value is an element of the type: nothing is rounded a second time.
+ *
+ * 16 tokens of one head in a page are a group, 17 head_dim bytes in one piece (all of
+ * them together 17/32 of a byte an element, keys and values):
+ *   key codes     [16 tokens][head_dim / 2]
+ *   value codes   [4][16 pieces][4 tokens][head_dim / 32]   piece n: elements n head_dim / 16
+ *                                                           .. (n + 1) head_dim / 16 - 1
+ *   key scales    [16 tokens][head_dim / 32]
+ *   value scales  [4][head_dim / 32][4 tokens]
+ * Group (page, head, g) begins at data + page * stride[0] + head * stride[1] +
+ * g * stride[2] (bytes). */
+typedef struct {
+  void* data;            /* 16-byte aligned                                      */
+  int64_t stride[3];     /* page, head, group of 16 tokens: multiples of 16 bytes */
+  int32_t n_pages;       /* >= 0                                                 */
+  int32_t page_size;     /* tokens per page: a power of two, 16 .. 65536         */
+  int32_t kv_heads;      /* 1 .. 1024                                            */
+  int32_t head_dim;      /* 64, 128 or 256 (ENOTIMPL otherwise)                  */
+  int32_t dtype;         /* of queries, outputs and what is read back            */
+  int32_t reserved;      /* 0                                                    */
+} fsched_kv4_cache;      /* 56 bytes */
+
+/* fsched_qk_norm_rope4 — fsched_qk_norm_rope into a cache of 4 bits.  Keys are normed
+ * and rotated in 64 bits and rounded once, to 4 bits; values are rounded as they are. */
+int fsched_qk_norm_rope4(const fsched_rope_params* p, const fsched_kv4_cache* kv,
+                         const void* qkv, const int32_t* positions, const int32_t* slots,
+                         const float* cos_sin, const void* q_weight, const void* k_weight,
+                         void* q_out, void* stream);
+
+/* fsched_kv4_read — tokens of a cache of 4 bits as elements: what the codes stand for,
+ * exactly (to move a request elsewhere, or to look at it).
+ *   n_tok           tokens
+ *   token_stride, head_stride  of k_out and v_out, elements
+ *   slots           [n_tok]; a slot outside the cache (-1) gives zeros
+ *   k_out, v_out    [n_tok][kv_heads][head_dim], 16-byte aligned */
+typedef struct {
+  int32_t n_tok;
+  uint32_t flags;
+  int64_t token_stride, head_stride;
+} fsched_read_params;
+
+int fsched_kv4_read(const fsched_read_params* p, const fsched_kv4_cache* kv,
+                    const int32_t* slots, void* k_out, void* v_out, void* stream);
+
+/* fsched_attend4 — fsched_attend (prefix_len 0) and fsched_attend_shared over a cache of 4
+ * bits: the same arguments, masks and results for the values that the codes stand for.
+ * prefix_pages is read only when prefix_len > 0. */
+int fsched_attend4(const fsched_attn_params* p, const fsched_kv4_cache* kv, const void* q,
+                   const int32_t* prefix_pages, const int32_t* table, const int32_t* q_start,
+                   const int32_t* kv_len, void* out, float* lse, void* workspace,
+                   int64_t workspace_bytes, void* stream);
+
+int fsched_attend4_workspace(const fsched_attn_params* p, const fsched_kv4_cache* kv,
+                             int64_t* bytes);
+
+/* fsched_attend_weight, fsched_attend4_weight — how much a step's new tokens look at each
+ * token that their request holds:
+ *   weight[r][j] += sum of exp(scale q.k_j - lse)
+ * over the new tokens of request r and the query heads that see key j, each with its row
+ * of lse, as the attention call of the same arguments returned it (a row whose lse is
+ * -infinity adds nothing).  Summed over steps and layers it says which tokens are used.
+ *   p               as in the attention call; the strides of out are not used, and with
+ *                   prefix_len > 0 the requests' own tokens are meant, behind the prefix,
+ *                   whose keys get no weight
+ *   kv              keys only: v may be NULL
+ *   lse             [n_tok][q_heads]
+ *   weight          in/out [n_req], rows weight_stride elements apart (>= table_width *
+ *                   page_size); entries of tokens that nobody sees stay as they were
+ * Results do not depend on the order in which the device runs the work.  The workspace is
+ * as for fsched_attend. */
+int fsched_attend_weight(const fsched_attn_params* p, const fsched_kv_cache* kv, const void* q,
+                         const float* lse, const int32_t* table, const int32_t* q_start,
+                         const int32_t* kv_len, float* weight, int64_t weight_stride,
+                         void* workspace, int64_t workspace_bytes, void* stream);
+
+int fsched_attend_weight_workspace(const fsched_attn_params* p, const fsched_kv_cache* kv,
+                                   int64_t* bytes);
+
+int fsched_attend4_weight(const fsched_attn_params* p, const fsched_kv4_cache* kv, const void* q,
+                          const float* lse, const int32_t* table, const int32_t* q_start,
+                          const int32_t* kv_len, float* weight, int64_t weight_stride,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+
+int fsched_attend4_weight_workspace(const fsched_attn_params* p, const fsched_kv4_cache* kv,
+                                    int64_t* bytes);
+
+/* fsched_kv_evict — whole pages given up, those of least weight first, until every request
+ * is within its budget.  Nothing in the cache moves: a request's row of the block table and
+ * its weights close up, and its later tokens keep their order.  (Rotations were applied
+ * when keys were stored, so a kept token keeps its position; a request's next token sits at
+ * new_len plus the tokens given up so far.)
+ *
+ * Request r holds len = kv_len[r] tokens (clamped to its row).  It gives up
+ *   min(ceil(max(0, len - budget[r]) / page_size), pages that it may give up)
+ * pages.  It may give up full pages behind the first ceil(n_sink / page_size) whose tokens
+ * all come before the last n_recent; those with the least sum of their tokens' weights (in
+ * 64 bits) go, of equal ones the earlier.
+ *   n_req, table_width, page_size   as elsewhere (page_size any power of two <= 65536)
+ *   n_sink, n_recent  first and last tokens that stay, >= 0
+ *   n_freed         capacity of freed
+ *   weight_stride   elements between rows of weight, >= table_width * page_size
+ *   weight          [n_req] rows, finite
+ *   budget          [n_req] tokens that each request may keep
+ *   new_table       [n_req][table_width] the pages that stay, in order; then -1
+ *   new_weight      [n_req][table_width * page_size] the weights of the tokens that stay;
+ *                   then 0.  Neither may overlap its input.
+ *   new_len         [n_req]
+ *   freed           [n_freed] ids of the pages given up (entries of the table below 0 are
+ *                   none), requests in order, pages in order; then -1
+ *   count           [1] pages given up with an id, also those beyond n_freed
+ *   workspace       as for fsched_attend */
+typedef struct {
+  int32_t n_req, table_width, page_size, n_sink, n_recent, n_freed;
+  uint32_t flags;
+  int32_t reserved; /* 0 */
+  int64_t weight_stride;
+} fsched_evict_params;
+
+int fsched_kv_evict(const fsched_evict_params* p, const float* weight, const int32_t* kv_len,
+                    const int32_t* table, const int32_t* budget, int32_t* new_table,
+                    float* new_weight, int32_t* new_len, int32_t* freed, int32_t* count,
+                    void* workspace, int64_t workspace_bytes, void* stream);
+
+int fsched_kv_evict_workspace(const fsched_evict_params* p, int64_t* bytes);
+
 /* Text for a return code (static storage). */
 const char* fsched_strerror(int code);
 

@@ -39,7 +39,10 @@ EXPORTS = ("fsched_simulate", "fsched_simulate_robust", "fsched_cost_decompose",
            "fsched_strerror", "fsched_abi_version", "fsched_last_hip_error",
            "fsched_release_cache", "fsched_simulate_noalloc", "fsched_kv_layout",
            "fsched_qk_norm_rope", "fsched_attend", "fsched_attend_shared",
-           "fsched_attend_workspace")
+           "fsched_attend_workspace", "fsched_qk_norm_rope4", "fsched_kv4_read",
+           "fsched_attend4", "fsched_attend4_workspace", "fsched_attend_weight",
+           "fsched_attend_weight_workspace", "fsched_attend4_weight",
+           "fsched_attend4_weight_workspace", "fsched_kv_evict", "fsched_kv_evict_workspace")
 
 
 class Params(ctypes.Structure):
@@ -80,8 +83,22 @@ def lib():
         L.fsched_attend.argtypes = [P] * 9 + [I64, P]
         L.fsched_attend_shared.argtypes = [P] * 10 + [I64, P]
         L.fsched_attend_workspace.argtypes = [P] * 3
+        L.fsched_qk_norm_rope4.argtypes = [P] * 10
+        L.fsched_kv4_read.argtypes = [P] * 6
+        L.fsched_attend4.argtypes = [P] * 10 + [I64, P]
+        L.fsched_attend4_workspace.argtypes = [P] * 3
+        L.fsched_attend_weight.argtypes = [P] * 8 + [I64, P, I64, P]
+        L.fsched_attend4_weight.argtypes = [P] * 8 + [I64, P, I64, P]
+        L.fsched_attend_weight_workspace.argtypes = [P] * 3
+        L.fsched_attend4_weight_workspace.argtypes = [P] * 3
+        L.fsched_kv_evict.argtypes = [P] * 11 + [I64, P]
+        L.fsched_kv_evict_workspace.argtypes = [P] * 2
         for f in (L.fsched_kv_layout, L.fsched_qk_norm_rope, L.fsched_attend,
-                  L.fsched_attend_shared, L.fsched_attend_workspace):
+                  L.fsched_attend_shared, L.fsched_attend_workspace, L.fsched_qk_norm_rope4,
+                  L.fsched_kv4_read, L.fsched_attend4, L.fsched_attend4_workspace,
+                  L.fsched_attend_weight, L.fsched_attend_weight_workspace,
+                  L.fsched_attend4_weight, L.fsched_attend4_weight_workspace,
+                  L.fsched_kv_evict, L.fsched_kv_evict_workspace):
             f.restype = ctypes.c_int
         for f in (L.fsched_simulate, L.fsched_simulate_noalloc, L.fsched_simulate_robust, L.fsched_cost_decompose, L.fsched_bruteforce_opt,
                   L.fsched_abi_version, L.fsched_last_hip_error, L.fsched_release_cache):
@@ -297,7 +314,9 @@ def bruteforce_opt(arrival, prompt, output, *, B: int, alpha: int, M_kv: int = 0
     return T, st
 
 
-_STEP = ("attend", "attend_shared", "attend_workspace", "kv_layout", "qk_norm_rope")
+_STEP = ("attend", "attend4", "attend4_weight", "attend4_workspace", "attend_shared",
+         "attend_weight", "attend_workspace", "kv4_cache", "kv4_read", "kv_evict", "kv_layout",
+         "qk_norm_rope", "qk_norm_rope4")
 
 
 def __getattr__(name):

@@ -1,5 +1,5 @@
 // Attention of a step's new tokens over the paged cache (fsched_attend,
-// fsched_attend_shared): which kernels a call runs, and the joining of parts.
+// fsched_attend_shared, fsched_attend4): which kernels a call runs, and the joining of parts.
 //
 //   rows blocks   requests with few rows (tokens times query heads per key head):
 //                 bound by the bytes of the cache
@@ -145,7 +145,7 @@ struct Shape {
 
 size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 
-Shape plan(const AttnArgs& a, int head_dim, int n_cu, char* ws) {
+Shape plan(const AttnArgs& a, bool fp4, int head_dim, int n_cu, char* ws) {
   Shape p;
   __builtin_memset((void*)&p, 0, sizeof(p));
   if (n_cu <= 0) n_cu = 256;
@@ -173,7 +173,7 @@ Shape plan(const AttnArgs& a, int head_dim, int n_cu, char* ws) {
     // beside tiles blocks one rows block per compute unit, else as many as fit
     p.main.rows_blocks = with_tiles || prefix
                              ? n_cu
-                             : n_cu * rows_occupancy(head_dim);
+                             : n_cu * rows_occupancy(head_dim, fp4);
     rp.waves = p.main.rows_blocks * ATT_WAVES;
     rp.keep_parts = prefix;
     rp.slot_rows = most < limit ? (int)most : limit;
@@ -234,11 +234,12 @@ Shape plan(const AttnArgs& a, int head_dim, int n_cu, char* ws) {
 }
 
 template <class T>
-hipError_t main_launch(const AttnArgs& a, const MainPlan& p, int head_dim, hipStream_t s) {
+hipError_t main_launch(const AttnArgs& a, bool fp4, const MainPlan& p, int head_dim,
+                       hipStream_t s) {
   switch (head_dim) {
-    case 64: return launch_main<T, 64>(a, p, s);
-    case 128: return launch_main<T, 128>(a, p, s);
-    default: return launch_main<T, 256>(a, p, s);
+    case 64: return fp4 ? launch_main4<T, 64>(a, p, s) : launch_main<T, 64>(a, p, s);
+    case 128: return fp4 ? launch_main4<T, 128>(a, p, s) : launch_main<T, 128>(a, p, s);
+    default: return fp4 ? launch_main4<T, 256>(a, p, s) : launch_main<T, 256>(a, p, s);
   }
 }
 
@@ -253,15 +254,15 @@ void join(const AttnArgs& a, const JoinArgs& j, int head_dim, dim3 grid, hipStre
 
 }  // namespace
 
-size_t attend_workspace(const AttnArgs& a, int head_dim, int n_cu) {
-  return plan(a, head_dim, n_cu, nullptr).bytes;
+size_t attend_workspace(const AttnArgs& a, bool fp4, int head_dim, int n_cu) {
+  return plan(a, fp4, head_dim, n_cu, nullptr).bytes;
 }
 
-hipError_t launch_attend(const AttnArgs& a, int dtype, int head_dim, int n_cu, void* workspace,
-                         hipStream_t s) {
-  const Shape p = plan(a, head_dim, n_cu, (char*)workspace);
-  const hipError_t e = dtype == FSCHED_BF16 ? main_launch<Bf16>(a, p.main, head_dim, s)
-                                            : main_launch<F16>(a, p.main, head_dim, s);
+hipError_t launch_attend(const AttnArgs& a, bool fp4, int dtype, int head_dim, int n_cu,
+                         void* workspace, hipStream_t s) {
+  const Shape p = plan(a, fp4, head_dim, n_cu, (char*)workspace);
+  const hipError_t e = dtype == FSCHED_BF16 ? main_launch<Bf16>(a, fp4, p.main, head_dim, s)
+                                            : main_launch<F16>(a, fp4, p.main, head_dim, s);
   if (e != hipSuccess || !p.joins) return e;
   // Enough blocks to fill the device, of 4 to 64 rows each.  Least rows of 1 / 4 / 16, us a
   // call: one request of 16,384 tokens 23 / 27 / 48, 33 drafting requests 25.8 / 25.7 /

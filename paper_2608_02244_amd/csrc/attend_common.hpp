@@ -25,6 +25,8 @@ constexpr int ATT_THREADS = 256, ATT_WAVES = ATT_THREADS / 64;
 // prompts 672 / 718 us a call, chunks beside decoding requests 109 / 111; decode alike (64
 // requests 55.6 / 55.1).
 constexpr int WIDE_SHIFT = 4;
+// What the cache's pages are: of fewer tokens than that, of 16 and more, or of 4 bits.
+enum { SMALL_PAGES = 0, WIDE_PAGES = 1, FP4_PAGES = 2 };
 constexpr float NEG_INF = -__builtin_inff();
 constexpr float LN2 = 0.6931471805599453f;
 

@@ -69,42 +69,51 @@ constexpr int MOST_PARTS = 128;
 //                  64 requests                                  - /  35 /  35 /  36
 //   heads of 256   64 requests, pages of 16 and of 8          108 / 117, 107 / 126
 //                  64 drafts; one request of 131,072 tokens   122 / 136, 218 / 211
-constexpr int rows_occupancy(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
+constexpr int rows_occupancy(int D, bool fp4) {
+  return fp4 ? (D == 256 ? 2 : 3) : D == 64 ? 3 : D == 128 ? 2 : 1;
+}
 
-// WIDE: pages of 16 tokens and more, so that keys 0..15 and 16..31 of a unit lie in
-// one page each and their addresses are uniform but for a lane's constant offset.
-template <class T, int D, int RT, bool WIDE>
-__device__ __forceinline__ void attend_rows(const AttnArgs& a, const RowsPlan& plan, int block,
-                                            char* lds) {
-  constexpr int KC = D / 32;   // 32-element chunks of a key
-  constexpr int DL = D / 16;   // elements of a value per lane
-  constexpr int VW = DL / 2;   // dwords of them
-  using elem = typename T::elem;
-  using x8 = typename T::x8;
+// The line of units and a wave's piece of it.
+struct RowsLine {
+  const int64_t* before;  // [n_req + 1] units before request r, of one key head (LDS)
+  int64_t per_head, total, waves;
+  int me;                 // this wave; at or past `waves`: without work
+  int64_t begin, end;     // its units
+
+  static __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+    // a 64-bit division is some 130 instructions
+    return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+  }
+  __device__ __forceinline__ int wave_of(int64_t unit) const {
+    return (int)quotient((unit + 1) * waves - 1, total);
+  }
+};
+
+__device__ __forceinline__ int rows_of(const AttnArgs& a, const Request& x) {
+  return min(x.q_len, a.max_q) * a.group;
+}
+
+__device__ __forceinline__ Span rows_span(const AttnArgs& a, const Request& x) {
+  const int p0 = x.kv - x.q_len;  // own index of the first token
+  return span_of<UNIT>(p0, p0 + min(x.q_len, a.max_q) - 1, x.kv, a.window, a.n_sink,
+                       a.prefix_len);
+}
+
+// Units before each request (a tile without a visible key is one unit all the same), and
+// the piece of this wave.  All threads of the block call it.
+__device__ __forceinline__ RowsLine rows_line(const AttnArgs& a, const RowsPlan& plan, int most,
+                                              int block, char* lds) {
   int64_t* wave_sum = (int64_t*)lds;  // [ATT_WAVES]
   int64_t* before = wave_sum + ATT_WAVES;  // [n_req + 1] units before request r
-
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int col = lane & 15, h = lane >> 4;
-  const int shift = a.kv.page_shift, page_mask = (1 << shift) - 1;
-
-  auto dims_of = [](int c) { return (c >> 1) * 64 + (c & 1) * 8; };
-  auto rows_of = [&](const Request& x) { return min(x.q_len, a.max_q) * a.group; };
-  auto mine = [&](const Request& x) { return x.q_len > 0 && rows_of(x) <= 16 * RT; };
-  auto span = [&](const Request& x) {
-    const int p0 = x.kv - x.q_len;  // own index of the first token
-    return span_of<UNIT>(p0, p0 + min(x.q_len, a.max_q) - 1, x.kv, a.window, a.n_sink,
-                         a.prefix_len);
-  };
-
-  // units before each request: a tile without a visible key is one unit all the same
+  auto mine = [&](const Request& x) { return x.q_len > 0 && rows_of(a, x) <= most; };
   {
     const int n = a.n_req, per = (n + ATT_THREADS - 1) / ATT_THREADS;
     const int r0 = min(n, tid * per), r1 = min(n, r0 + per);
     int64_t sum = 0;
     for (int r = r0; r < r1; ++r) {
       const Request x = request_of(a, r);
-      const int u = mine(x) ? max(1, span(x).blocks) : 0;
+      const int u = mine(x) ? max(1, rows_span(a, x).blocks) : 0;
       before[r] = u;
       sum += u;
     }
@@ -126,36 +135,125 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const RowsPlan& p
     if (tid == ATT_THREADS - 1) before[n] = at;
     __syncthreads();
   }
-  const int64_t per_head = before[a.n_req];
-  const int64_t total = per_head * a.kv.kv_heads;
-  auto quotient = [](int64_t x, int64_t y) {  // a 64-bit division is some 130 instructions
-    return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
-  };
+  RowsLine l;
+  l.before = before;
+  l.per_head = before[a.n_req];
+  l.total = l.per_head * a.kv.kv_heads;
   // Waves with work: a few tiles are not cut finer than their parts are worth reading
   // again.  Wave i takes units i total / waves .. (i + 1) total / waves.
-  const int64_t waves = min(min((int64_t)plan.waves, total),
-                            (int64_t)MOST_PARTS * a.n_req * a.kv.kv_heads);
-  const int me = uni_int(block * ATT_WAVES + wave);
-  if (me >= waves) return;
-  const int64_t begin = quotient(me * total, waves), end = quotient((me + 1) * total, waves);
-  auto wave_of = [&](int64_t unit) { return (int)quotient((unit + 1) * waves - 1, total); };
+  l.waves = min(min((int64_t)plan.waves, l.total), (int64_t)MOST_PARTS * a.n_req * a.kv.kv_heads);
+  l.me = uni_int(block * ATT_WAVES + wave);
+  l.begin = l.end = 0;
+  if (l.me < l.waves) {
+    l.begin = RowsLine::quotient(l.me * l.total, l.waves);
+    l.end = RowsLine::quotient((l.me + 1) * l.total, l.waves);
+  }
+  return l;
+}
 
-  for (int64_t w = begin; w < end;) {
-    const int kh = (int)quotient(w, per_head);
-    const int64_t rest = w - kh * per_head;
-    int lo = 0, hi = a.n_req;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (before[mid] <= rest) lo = mid;
-      else hi = mid;
+// The tile of a unit, and what of it lies in the wave's piece.
+struct RowsPart {
+  int kh, r, units, u0, u1;  // units u0 .. u1 of the tile's `units`
+};
+
+__device__ __forceinline__ RowsPart rows_part(const AttnArgs& a, const RowsLine& l, int64_t w) {
+  RowsPart p;
+  p.kh = (int)RowsLine::quotient(w, l.per_head);
+  const int64_t rest = w - p.kh * l.per_head;
+  int lo = 0, hi = a.n_req;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (l.before[mid] <= rest) lo = mid;
+    else hi = mid;
+  }
+  p.r = lo;
+  p.units = (int)(l.before[lo + 1] - l.before[lo]);
+  p.u0 = (int)(rest - l.before[lo]);
+  p.u1 = (int)min((int64_t)p.units, p.u0 + (l.end - w));
+  return p;
+}
+
+// A part's end: the result of a tile that lies whole in the wave's piece, else a part for
+// the join.  A lane holds 4 DL neighbouring elements of its rows, from 4 DL h on.
+template <class T, int D, int RT>
+__device__ __forceinline__ void rows_write(const AttnArgs& a, const RowsPlan& plan,
+                                           const RowsLine& line, const RowsPart& at_unit,
+                                           int64_t w, const Request& x, int rows,
+                                           const f32x4 (&o)[RT][D / 16], const float (&mu)[RT],
+                                           const float (&l)[RT]) {
+  constexpr int DL = D / 16;
+  using elem = typename T::elem;
+  const int lane = threadIdx.x & 63, col = lane & 15, h = lane >> 4, kh = at_unit.kh;
+  const bool whole = at_unit.u0 == 0 && at_unit.u1 == at_unit.units;
+  const int64_t tile = (int64_t)kh * a.n_req + at_unit.r;
+  const int64_t slot = whole && plan.keep_parts ? 2 * (int64_t)plan.waves + tile
+                                                : 2 * (int64_t)line.me + (w != line.begin);
+  if (at_unit.u0 == 0 && lane == 0) {
+    RowsTile d;
+    d.first = (int32_t)slot;
+    d.wave = line.me;
+    d.count = line.wave_of(w + at_unit.units - 1) - line.me + 1;
+    d.pad = 0;
+    plan.tiles[tile] = d;
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int row = t * 16 + col;
+    const float sum = sum_xor32(sum_xor16(l[t]));
+    if (row >= rows) continue;
+    if (whole && !plan.keep_parts) {
+      const int tok = row / a.group, qh = kh * a.group + row - tok * a.group;
+      const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
+      uint32_t y[2 * DL];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 0; d < DL; d += 2)
+          y[(i * DL + d) / 2] = pack2<T>(o[t][d][i] * inv, o[t][d + 1][i] * inv);
+      elem* dst = (elem*)a.out + (int64_t)(x.q0 + tok) * a.o_token + (int64_t)qh * a.o_head +
+                  4 * DL * h;
+#pragma unroll
+      for (int i = 0; i < 2 * DL; i += 4)
+        *(u32x4*)(dst + 2 * i) = (u32x4){y[i], y[i + 1], y[i + 2], y[i + 3]};
+      if (a.lse && h == 0)
+        a.lse[(int64_t)(x.q0 + tok) * a.q_heads + qh] = (mu[t] + log2f(sum)) * LN2;
+    } else {
+      const int64_t at = slot * plan.slot_rows + row;
+      float* dst = plan.part_o + at * D + 4 * DL * h;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 0; d < DL; d += 4)
+          *(f32x4*)(dst + i * DL + d) =
+              (f32x4){o[t][d][i], o[t][d + 1][i], o[t][d + 2][i], o[t][d + 3][i]};
+      if (h == 0) plan.part_ml[at] = make_float2(mu[t], sum);
     }
-    const int r = lo;
-    const int units = (int)(before[r + 1] - before[r]);
-    const int u0 = (int)(rest - before[r]);
-    const int u1 = (int)min((int64_t)units, u0 + (end - w));
+  }
+}
+
+// WIDE: pages of 16 tokens and more, so that keys 0..15 and 16..31 of a unit lie in
+// one page each and their addresses are uniform but for a lane's constant offset.
+template <class T, int D, int RT, bool WIDE>
+__device__ __forceinline__ void attend_rows(const AttnArgs& a, const RowsPlan& plan, int block,
+                                            char* lds) {
+  constexpr int KC = D / 32;   // 32-element chunks of a key
+  constexpr int DL = D / 16;   // elements of a value per lane
+  constexpr int VW = DL / 2;   // dwords of them
+  using elem = typename T::elem;
+  using x8 = typename T::x8;
+  const int lane = threadIdx.x & 63;
+  const int col = lane & 15, h = lane >> 4;
+  const int shift = a.kv.page_shift, page_mask = (1 << shift) - 1;
+  auto dims_of = [](int c) { return (c >> 1) * 64 + (c & 1) * 8; };
+
+  const RowsLine line = rows_line(a, plan, 16 * RT, block, lds);
+  if (line.me >= line.waves) return;
+  for (int64_t w = line.begin; w < line.end;) {
+    const RowsPart part = rows_part(a, line, w);
+    const int kh = part.kh, r = part.r, u0 = part.u0, u1 = part.u1;
     const Request x = request_of(a, r);
-    const Span sp = span(x);
-    const int rows = rows_of(x);
+    const Span sp = rows_span(a, x);
+    const int rows = rows_of(a, x);
     const int first_own = x.kv - x.q_len;           // own index of the first token
     const int last_own = first_own + min(x.q_len, a.max_q) - 1;
     const int n_keys = min(x.kv, last_own + 1);     // keys past it are seen by none
@@ -343,52 +441,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, const RowsPlan& p
       }
     }
 
-    const bool whole = u0 == 0 && u1 == units;
-    const int64_t tile = (int64_t)kh * a.n_req + r;
-    const int64_t slot =
-        whole && plan.keep_parts ? 2 * (int64_t)plan.waves + tile : 2 * (int64_t)me + (w != begin);
-    if (u0 == 0 && lane == 0) {
-      RowsTile d;
-      d.first = (int32_t)slot;
-      d.wave = me;
-      d.count = wave_of(w + units - 1) - me + 1;
-      d.pad = 0;
-      plan.tiles[tile] = d;
-    }
-    // a lane holds 4 DL neighbouring elements of its row, from 4 DL h on
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int row = t * 16 + col;
-      const float sum = sum_xor32(sum_xor16(l[t]));
-      if (row >= rows) continue;
-      if (whole && !plan.keep_parts) {
-        const int tok = row / a.group, qh = kh * a.group + row - tok * a.group;
-        const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
-        uint32_t y[2 * DL];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int d = 0; d < DL; d += 2)
-            y[(i * DL + d) / 2] = pack2<T>(o[t][d][i] * inv, o[t][d + 1][i] * inv);
-        elem* dst = (elem*)a.out + (int64_t)(x.q0 + tok) * a.o_token + (int64_t)qh * a.o_head +
-                    4 * DL * h;
-#pragma unroll
-        for (int i = 0; i < 2 * DL; i += 4)
-          *(u32x4*)(dst + 2 * i) = (u32x4){y[i], y[i + 1], y[i + 2], y[i + 3]};
-        if (a.lse && h == 0)
-          a.lse[(int64_t)(x.q0 + tok) * a.q_heads + qh] = (mu[t] + log2f(sum)) * LN2;
-      } else {
-        const int64_t at = slot * plan.slot_rows + row;
-        float* dst = plan.part_o + at * D + 4 * DL * h;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int d = 0; d < DL; d += 4)
-            *(f32x4*)(dst + i * DL + d) =
-                (f32x4){o[t][d][i], o[t][d + 1][i], o[t][d + 2][i], o[t][d + 3][i]};
-        if (h == 0) plan.part_ml[at] = make_float2(mu[t], sum);
-      }
-    }
+    rows_write<T, D, RT>(a, plan, line, part, w, x, rows, o, mu, l);
     w += u1 - u0;
   }
 }

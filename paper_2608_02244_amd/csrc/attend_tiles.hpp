@@ -24,6 +24,7 @@
 #include <hip/hip_runtime.h>
 
 #include "attend_common.hpp"
+#include "fp4.hpp"
 
 namespace fs {
 
@@ -100,6 +101,10 @@ __device__ __forceinline__ void write16(uint32_t addr, u32x4 v) {
   *(__attribute__((address_space(3))) u32x4*)(uintptr_t)addr = v;
 }
 
+__device__ __forceinline__ void write8(uint32_t addr, u32x2 v) {
+  *(__attribute__((address_space(3))) u32x2*)(uintptr_t)addr = v;
+}
+
 __device__ __forceinline__ uint64_t lane_of(uint64_t x, int lane) {
   const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, lane);
   const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane);
@@ -111,13 +116,25 @@ __device__ __forceinline__ uint64_t shuffled(uint64_t x, int lane) {
   return (uint64_t)hi << 32 | lo;
 }
 
-// WIDE: pages of 16 tokens and more.  The keys that a wave loads at once (8, 4 or 2,
-// from a multiple of that on) then lie in one page, and their addresses are uniform but
-// for a lane's constant offset.
-template <class T, int D, bool WIDE>
+// A thread's share of a tile in 4 bits: D / (256 / KEYS) elements of one key, and as many of
+// the values (a piece's, of the four tokens of a quarter of a group, or half of it).
+template <int D>
+struct Tile4 {
+  static constexpr int SHARE = ATT_THREADS / Tile<D>::KEYS;  // threads of a key
+  static constexpr int WORDS = D / SHARE / 8;                // dwords of codes each side
+  uint32_t k[WORDS], v[WORDS], k_scale, v_scale;             // scales as loaded
+};
+
+// KIND SMALL_PAGES, WIDE_PAGES (of 16 tokens and more: the keys that a wave loads at once,
+// 8, 4 or 2 from a multiple of that on, then lie in one page, and their addresses are
+// uniform but for a lane's constant offset) or FP4_PAGES (a cache of 4 bits: the tile goes
+// through registers, where its codes become elements, into the same places in LDS; loaded
+// two tiles ahead, converted one ahead).
+template <class T, int D, int KIND>
 __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan& plan, int block,
                                              char* lds) {
   using L = Tile<D>;
+  constexpr bool WIDE = KIND == WIDE_PAGES, FP4 = KIND == FP4_PAGES;
   constexpr int KB = L::KEYS, NT = KB / 32, QC = D / 16, DT = D / 32;
   using elem = typename T::elem;
   using x8 = typename T::x8;
@@ -183,9 +200,91 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
     }
   };
 
-  int page = 0, page_next = 0;
+  // The same for 4 bits: this thread's share of tile b, and its elements to buffer `buf`.
+  using Raw = Tile4<D>;
+  using G = Group4<D>;
+  constexpr int KEY_SHARE = D / Raw::SHARE;  // elements of a key that a thread converts
+  const int my_key = tid / Raw::SHARE, my_block = tid % Raw::SHARE * KEY_SHARE / 32;
+  // values: token quarter of a group (of 4 tokens), piece, and for D = 256 which two of them
+  const int my_quarter = D == 256 ? tid >> 5 : tid >> 4;
+  const int my_piece = D == 256 ? (tid & 31) >> 1 : tid & 15, my_half = D == 256 ? tid & 1 : 0;
+  auto load4 = [&](int b, int pages) {
+    Raw t;
+    const int s0 = sp.block(b) * KB;
+    auto group_of = [&](int key) {
+      const int mine = __shfl(pages, key);  // lane j has the page of key j
+      const uint32_t pg = in_cache(mine) ? mine : 0, slot = (s0 + key) & page_mask;
+      return (const char*)a.kv.k + pg * (uint64_t)a.kv.k_page + kh * a.kv.k_head +
+             (slot >> GROUP_SHIFT) * (uint64_t)a.kv.k_slot;
+    };
+    const char* kg = group_of(my_key);
+    const char* vg = group_of(my_quarter * 4);
+    const int kt = my_key & (GROUP - 1), vt = my_quarter * 4 & (GROUP - 1);
+    const uint32_t* kp = (const uint32_t*)(kg + G::key(kt) + tid % Raw::SHARE * (KEY_SHARE / 2));
+    const uint32_t* vp = (const uint32_t*)(vg + G::value(vt, my_piece) + my_half * 16);
+    if constexpr (Raw::WORDS == 4) {
+      const u32x4 x = *(const u32x4*)kp, y = *(const u32x4*)vp;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) t.k[i] = x[i], t.v[i] = y[i];
+    } else {
+      const u32x2 x = *(const u32x2*)kp, y = *(const u32x2*)vp;
+      t.k[0] = x[0], t.k[1] = x[1], t.v[0] = y[0], t.v[1] = y[1];
+    }
+    t.k_scale = *(const uint8_t*)(kg + G::key_scale(kt, my_block));
+    t.v_scale = *(const uint32_t*)(vg + G::value_scale(vt, my_piece * (D / 16) / 32));
+    return t;
+  };
+  auto store4 = [&](const Raw& t, int buf) {
+    const uint32_t to = lds0 + buf * (2 * L::BYTES);
+    auto place = [&](int key, int piece) {
+      return to + key * (D * 2) + (piece ^ L::swizzle(key)) * 16;
+    };
+    const float ks = scale_of(t.k_scale);
+#pragma unroll
+    for (int i = 0; i < Raw::WORDS; ++i)
+      write16(place(my_key, tid % Raw::SHARE * Raw::WORDS + i), values8<T>(t.k[i], ks));
+    const int key = my_quarter * 4;
+    auto scale = [&](int j) { return scale_of((t.v_scale >> (8 * j)) & 255); };
+    if constexpr (D == 64) {  // two bytes of each token: half a 16-byte piece
+      const uint32_t at = L::BYTES + (my_piece & 1) * 8;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t c = t.v[j >> 1];
+        const float s = scale(j);
+        const u32x2 y = j & 1 ? (u32x2){values2<T, 2>(c, s), values2<T, 3>(c, s)}
+                              : (u32x2){values2<T, 0>(c, s), values2<T, 1>(c, s)};
+        write8(place(key + j, my_piece >> 1) + at, y);
+      }
+    } else if constexpr (D == 128) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        write16(place(key + j, my_piece) + L::BYTES, values8<T>(t.v[j], scale(j)));
+    } else {  // 8 bytes of two tokens
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float s = scale_of((t.v_scale >> (16 * my_half + 8 * j)) & 255);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          write16(place(key + 2 * my_half + j, 2 * my_piece + i) + L::BYTES,
+                  values8<T>(t.v[2 * j + i], s));
+      }
+    }
+  };
+
+  int page = 0, page_next = 0, page_far = 0;
+  Raw raw;
   auto first_fetch = [&]() {
     if (b0 >= b1) return;
+    if constexpr (FP4) {
+      page = page_at(b0);
+      store4(load4(b0, page), 0);
+      if (b0 + 1 < b1) {
+        page_next = page_at(b0 + 1);
+        raw = load4(b0 + 1, page_next);
+      }
+      if (b0 + 2 < b1) page_far = page_at(b0 + 2);
+      return;
+    }
     page = page_at(b0);
     fetch(b0, page, 0);
     if (b0 + 1 < b1) page_next = page_at(b0 + 1);
@@ -371,12 +470,20 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
 
   for (int b = b0; b < b1; ++b) {
     const int buf = (b - b0) & 1;
-    wait_loads();
+    if constexpr (!FP4) wait_loads();
     __syncthreads();  // tile b is there; the other buffer is free
     const uint64_t found = __ballot(seen(key_at(b)) && in_cache(page));
-    if (b + 1 < b1) fetch(b + 1, page_next, buf ^ 1);
-    page = page_next;
-    if (b + 2 < b1) page_next = page_at(b + 2);
+    if constexpr (FP4) {
+      if (b + 1 < b1) store4(raw, buf ^ 1);
+      if (b + 2 < b1) raw = load4(b + 2, page_far);
+      page = page_next;
+      page_next = page_far;
+      if (b + 3 < b1) page_far = page_at(b + 3);
+    } else {
+      if (b + 1 < b1) fetch(b + 1, page_next, buf ^ 1);
+      page = page_next;
+      if (b + 2 < b1) page_next = page_at(b + 2);
+    }
 
     const int s0 = sp.block(b) * KB;
     const uint32_t shift_b = buf * (2 * L::BYTES);

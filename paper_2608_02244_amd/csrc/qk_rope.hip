@@ -1,6 +1,7 @@
 // Norms of queries and keys per head, their rotation, and the store of keys and
 // values into the cache, in one pass over the fused projection
-// (fsched_qk_norm_rope).
+// (fsched_qk_norm_rope), of 16 bits or of 4 (fsched_qk_norm_rope4), and the read back of
+// the latter (fsched_kv4_read).
 //
 //   y = x / sqrt(mean(x^2) + eps) * w;  (a, b) -> (a cos - b sin, b cos + a sin)
 //
@@ -12,9 +13,13 @@
 // and kept for all the heads that the wave takes of it.
 // Measured: 32,771 tokens of 48 heads of 128 (f16), 163 us or 5.0 TB/s, a large copy's
 // rate; 64 tokens, 3.7 us.
+//
+// Into a cache of 4 bits, keys are normed and rotated in 64 bits, so that their codes are
+// those of the numbers themselves and not of one order of summing them: a number next to
+// the border of two codes is off by a third of itself on the other side.
 #include <hip/hip_runtime.h>
 
-#include "half.hpp"
+#include "fp4.hpp"
 #include "step_common.hpp"
 
 namespace fs {
@@ -22,7 +27,53 @@ namespace {
 
 constexpr int THREADS = 256;
 
+// A key in 64 bits: normed (weight given) and rotated (c, s given) as the kernel below does.
 template <class T, int D, bool INTER>
+__device__ __forceinline__ void exact_key(typename T::x8 raw, const void* weight, float eps,
+                                          bool turns, bool rotated, const float* c,
+                                          const float* s, int d0, int partner, float* out) {
+  using x8 = typename T::x8;
+  using elem = typename T::elem;
+  double x[8], sq = 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[i] = (double)(float)raw[i];
+    sq = fma(x[i], x[i], sq);
+  }
+  if (weight) {
+#pragma unroll
+    for (int d = 1; d < D / 8; d <<= 1) sq += __shfl_xor(sq, d);
+    const double r = 1.0 / sqrt(sq * (1.0 / D) + (double)eps);
+    const x8 g = *(const x8*)((const elem*)weight + d0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (double)(float)g[i];
+  }
+  if (turns) {
+    if (INTER) {
+      if (rotated) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const double p = x[2 * i], q = x[2 * i + 1];
+          x[2 * i] = p * (double)c[i] - q * (double)s[i];
+          x[2 * i + 1] = q * (double)c[i] + p * (double)s[i];
+        }
+      }
+    } else {
+      double y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = __shfl(x[i], partner & 63);
+      if (rotated) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * (double)c[i] + y[i] * (double)s[i];
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) out[i] = to_odd(x[i]);
+}
+
+// FP4: the cache holds 4 bits an element; its strides are bytes, k_slot that of a group.
+template <class T, int D, bool INTER, bool FP4>
 __global__ __launch_bounds__(THREADS) void qk_rope_kernel(RopeArgs a, int chunks, int per_chunk) {
   constexpr int LANES = D / 8;        // lanes of one head vector
   constexpr int HEADS = 64 / LANES;   // head vectors a wave holds at once
@@ -122,6 +173,40 @@ __global__ __launch_bounds__(THREADS) void qk_rope_kernel(RopeArgs a, int chunks
     if (is_q) {
       const x8 zero = {};
       *(x8*)((elem*)a.q_out + t * a.q_token + (int64_t)h * a.q_head + d0) = known ? res : zero;
+    } else if constexpr (FP4) {
+      if (!store) continue;  // a head's lanes alike
+      using G = Group4<D>;
+      float y[8];
+      if (is_k) {
+        exact_key<T, D, INTER>(raw, weight, a.eps, a.rot_dim > 0, rotated, c, s, d0, partner, y);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = (float)raw[i];
+      }
+      uint32_t top = 0;  // as whole numbers, in which NaN and infinity are above all others
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        top = max(top, __builtin_bit_cast(uint32_t, y[i]) & 0x7fffffffu);
+      top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+      const int byte = scale_byte<T>(top);
+      const uint32_t code = byte == 255 ? 0 : codes8(y, scale_of(byte));
+      const int64_t kh = h - a.q_heads - (is_k ? 0 : a.kv.kv_heads);
+      char* group = (char*)const_cast<void*>(a.kv.k) + page * a.kv.k_page + kh * a.kv.k_head +
+                    (off >> GROUP_SHIFT) * a.kv.k_slot;
+      const int tok = off & (GROUP - 1);
+      if (is_k) {
+        *(uint32_t*)(group + G::key(tok) + sub * 4) = code;
+      } else if constexpr (D == 64) {  // two pieces of 4 elements
+        *(uint16_t*)(group + G::value(tok, 2 * sub)) = (uint16_t)code;
+        *(uint16_t*)(group + G::value(tok, 2 * sub + 1)) = (uint16_t)(code >> 16);
+      } else {
+        constexpr int PER = D / 128;  // lanes of a piece
+        *(uint32_t*)(group + G::value(tok, sub / PER) + sub % PER * 4) = code;
+      }
+      if ((sub & 3) == 0)
+        *(uint8_t*)(group + (is_k ? G::key_scale(tok, sub >> 2) : G::value_scale(tok, sub >> 2))) =
+            (uint8_t)byte;
     } else if (store) {
       const int64_t kh = h - a.q_heads - (is_k ? 0 : a.kv.kv_heads);
       const int64_t at = is_k ? page * a.kv.k_page + kh * a.kv.k_head + off * a.kv.k_slot
@@ -132,7 +217,53 @@ __global__ __launch_bounds__(THREADS) void qk_rope_kernel(RopeArgs a, int chunks
   }
 }
 
+// A lane has 8 elements of one token, head and side.
 template <class T, int D>
+__global__ __launch_bounds__(THREADS) void kv4_read_kernel(Read4Args a) {
+  using G = Group4<D>;
+  using elem = typename T::elem;
+  constexpr int LANES = D / 8;
+  const int64_t at = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+  const int sub = (int)(at % LANES);
+  const int64_t v = at / LANES;  // token, side, head
+  const int kh = (int)(v % a.kv.kv_heads), side = (int)(v / a.kv.kv_heads & 1);
+  const int64_t t = v / a.kv.kv_heads >> 1;
+  if (t >= a.n_tok) return;
+  const int slot = a.slots[t], page = slot >> a.kv.page_shift;
+  const int off = slot & ((1 << a.kv.page_shift) - 1), tok = off & (GROUP - 1);
+  u32x4 x = {0, 0, 0, 0};
+  if (slot >= 0 && page < a.kv.n_pages) {
+    const char* group = (const char*)a.kv.k + page * a.kv.k_page + kh * a.kv.k_head +
+                        (off >> GROUP_SHIFT) * a.kv.k_slot;
+    uint32_t code;
+    if (side == 0) {
+      code = *(const uint32_t*)(group + G::key(tok) + sub * 4);
+    } else if constexpr (D == 64) {
+      code = *(const uint16_t*)(group + G::value(tok, 2 * sub)) |
+             (uint32_t)*(const uint16_t*)(group + G::value(tok, 2 * sub + 1)) << 16;
+    } else {
+      constexpr int PER = D / 128;
+      code = *(const uint32_t*)(group + G::value(tok, sub / PER) + sub % PER * 4);
+    }
+    const int byte = *(const uint8_t*)(group + (side == 0 ? G::key_scale(tok, sub >> 2)
+                                                          : G::value_scale(tok, sub >> 2)));
+    x = values8<T>(code, scale_of(byte));
+    if (byte == 255) {  // NaN
+      const uint32_t nan = pack2<T>(__builtin_nanf(""), __builtin_nanf(""));
+      x = (u32x4){nan, nan, nan, nan};
+    }
+  }
+  elem* out = (elem*)(side == 0 ? a.k_out : a.v_out);
+  *(u32x4*)(out + t * a.token + kh * a.head + sub * 8) = x;
+}
+
+template <class T, int D>
+void read(const Read4Args& a, hipStream_t s) {
+  const int64_t lanes = (int64_t)a.n_tok * a.kv.kv_heads * 2 * (D / 8);
+  kv4_read_kernel<T, D><<<dim3((unsigned)((lanes + THREADS - 1) / THREADS)), THREADS, 0, s>>>(a);
+}
+
+template <class T, int D, bool FP4>
 hipError_t launch(const RopeArgs& a, int n_cu, hipStream_t s) {
   const int heads = a.q_heads + 2 * a.kv.kv_heads, at_once = 64 / (D / 8);
   // All heads of a token in one wave (its rotation row is loaded once), unless
@@ -147,25 +278,45 @@ hipError_t launch(const RopeArgs& a, int n_cu, hipStream_t s) {
   chunks = (heads + per - 1) / per;
   const int64_t waves = (int64_t)a.n_tok * chunks;
   const dim3 grid((unsigned)((waves + THREADS / 64 - 1) / (THREADS / 64))), block(THREADS);
-  if (a.interleaved) qk_rope_kernel<T, D, true><<<grid, block, 0, s>>>(a, chunks, per);
-  else qk_rope_kernel<T, D, false><<<grid, block, 0, s>>>(a, chunks, per);
+  if (a.interleaved) qk_rope_kernel<T, D, true, FP4><<<grid, block, 0, s>>>(a, chunks, per);
+  else qk_rope_kernel<T, D, false, FP4><<<grid, block, 0, s>>>(a, chunks, per);
   return hipGetLastError();
 }
 
-template <class T>
+template <class T, bool FP4>
 hipError_t launch_dim(const RopeArgs& a, int head_dim, int n_cu, hipStream_t s) {
   switch (head_dim) {
-    case 64: return launch<T, 64>(a, n_cu, s);
-    case 128: return launch<T, 128>(a, n_cu, s);
-    default: return launch<T, 256>(a, n_cu, s);
+    case 64: return launch<T, 64, FP4>(a, n_cu, s);
+    case 128: return launch<T, 128, FP4>(a, n_cu, s);
+    default: return launch<T, 256, FP4>(a, n_cu, s);
+  }
+}
+
+template <class T>
+void read_dim(const Read4Args& a, int head_dim, hipStream_t s) {
+  switch (head_dim) {
+    case 64: return read<T, 64>(a, s);
+    case 128: return read<T, 128>(a, s);
+    default: return read<T, 256>(a, s);
   }
 }
 
 }  // namespace
 
 hipError_t launch_qk_rope(const RopeArgs& a, int dtype, int head_dim, int n_cu, hipStream_t s) {
-  return dtype == FSCHED_BF16 ? launch_dim<Bf16>(a, head_dim, n_cu, s)
-                              : launch_dim<F16>(a, head_dim, n_cu, s);
+  return dtype == FSCHED_BF16 ? launch_dim<Bf16, false>(a, head_dim, n_cu, s)
+                              : launch_dim<F16, false>(a, head_dim, n_cu, s);
+}
+
+hipError_t launch_qk_rope4(const RopeArgs& a, int dtype, int head_dim, int n_cu, hipStream_t s) {
+  return dtype == FSCHED_BF16 ? launch_dim<Bf16, true>(a, head_dim, n_cu, s)
+                              : launch_dim<F16, true>(a, head_dim, n_cu, s);
+}
+
+hipError_t launch_kv4_read(const Read4Args& a, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == FSCHED_BF16) read_dim<Bf16>(a, head_dim, s);
+  else read_dim<F16>(a, head_dim, s);
+  return hipGetLastError();
 }
 
 }  // namespace fs

@@ -1,5 +1,5 @@
 // Launch descriptors and host checks shared by the operators of a step
-// (kv_layout.hip, qk_rope.hip, attend*.hip, step_abi.cpp).
+// (kv_layout.hip, qk_rope.hip, attend*.hip, kv_evict.hip, step_abi.cpp).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -21,7 +21,9 @@ struct LayoutArgs {
   int32_t* used;
 };
 
-struct CacheRef {  // device view of an fsched_kv_cache
+// Device view of an fsched_kv_cache, or of an fsched_kv4_cache: then k is its data and
+// k_page, k_head and k_slot (of a group of 16 tokens) are bytes; the v fields are unused.
+struct CacheRef {
   const void* k;
   const void* v;
   int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
@@ -42,6 +44,15 @@ struct RopeArgs {
   void* q_out;
 };
 
+struct Read4Args {
+  int32_t n_tok;
+  int64_t token, head;
+  CacheRef kv;
+  const int32_t* slots;
+  void* k_out;
+  void* v_out;
+};
+
 struct AttnArgs {
   int32_t n_req, n_tok, q_heads, group, max_q, width, window, n_sink, prefix_len;
   float scale_log2;  // scale * log2(e): exponentials are taken in base 2
@@ -56,12 +67,44 @@ struct AttnArgs {
   float* lse;  // nullable
 };
 
+// The attention weight of held tokens: of `at` q, the tables and the cache's keys.
+struct WeightArgs {
+  AttnArgs at;
+  const float* lse;
+  float* weight;
+  int64_t weight_stride;
+};
+
+struct EvictArgs {
+  int32_t n_req, width, page_shift, n_sink, n_recent, n_freed;
+  int64_t weight_stride;
+  const float* weight;
+  const int32_t* kv_len;
+  const int32_t* table;
+  const int32_t* budget;
+  int32_t* new_table;
+  float* new_weight;
+  int32_t* new_len;
+  int32_t* freed;
+  int32_t* count;
+};
+
 hipError_t launch_kv_layout(const LayoutArgs& a, hipStream_t s);
 hipError_t launch_qk_rope(const RopeArgs& a, int dtype, int head_dim, int n_cu, hipStream_t s);
+hipError_t launch_qk_rope4(const RopeArgs& a, int dtype, int head_dim, int n_cu, hipStream_t s);
+hipError_t launch_kv4_read(const Read4Args& a, int dtype, int head_dim, hipStream_t s);
 
-// Workspace bytes of one attention call on a device of n_cu compute units.
-size_t attend_workspace(const AttnArgs& a, int head_dim, int n_cu);
-hipError_t launch_attend(const AttnArgs& a, int dtype, int head_dim, int n_cu, void* workspace,
-                         hipStream_t s);
+// Workspace bytes of one attention call on a device of n_cu compute units.  fp4: over a
+// cache of 4 bits.
+size_t attend_workspace(const AttnArgs& a, bool fp4, int head_dim, int n_cu);
+hipError_t launch_attend(const AttnArgs& a, bool fp4, int dtype, int head_dim, int n_cu,
+                         void* workspace, hipStream_t s);
+
+size_t weight_workspace(const WeightArgs& a, bool fp4, int head_dim, int n_cu);
+hipError_t launch_weight(const WeightArgs& a, bool fp4, int dtype, int head_dim, int n_cu,
+                         void* workspace, hipStream_t s);
+
+size_t evict_workspace(const EvictArgs& a);
+hipError_t launch_evict(const EvictArgs& a, int n_cu, void* workspace, hipStream_t s);
 
 }  // namespace fs

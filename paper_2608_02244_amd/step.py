@@ -1,8 +1,11 @@
 """The operators of a serving step: KV placement, norm and rotation of queries and
-keys with the store into the cache, and attention over the paged cache.
+keys with the store into the cache, and attention over the paged cache; the same over a
+cache of 4 bits, the attention weight of held tokens, and pages given up by it.
 
-Binding of ``fsched_kv_layout``, ``fsched_qk_norm_rope``, ``fsched_attend`` and
-``fsched_attend_shared`` (``include/fsched.h`` says what each computes).  Every
+Binding of ``fsched_kv_layout``, ``fsched_qk_norm_rope``, ``fsched_attend``,
+``fsched_attend_shared``, ``fsched_qk_norm_rope4``, ``fsched_kv4_read``,
+``fsched_attend4``, ``fsched_attend_weight``, ``fsched_attend4_weight`` and
+``fsched_kv_evict`` (``include/fsched.h`` says what each computes).  Every
 array is a torch tensor, all of a call's on one GPU; the calls are enqueued on the
 current torch stream and nothing is synchronised.  They are for serving: no gradient
 flows through them.
@@ -14,7 +17,8 @@ the tensors' device (ValueError).
 
 A cache is a pair of tensors [n_pages, kv_heads, page_size, head_dim]; a permuted
 view (another order of page, head and slot in memory) does as well, as long as the
-head dimension is contiguous.
+head dimension is contiguous.  A cache of 4 bits is one uint8 tensor [n_pages, kv_heads,
+page_size / 16, 17 head_dim] (``kv4_cache`` makes one) that holds keys and values.
 """
 from __future__ import annotations
 
@@ -42,6 +46,11 @@ class KvCache(ctypes.Structure):
                 ("dtype", _I32), ("reserved", _I32)]
 
 
+class Kv4Cache(ctypes.Structure):
+    _fields_ = [("data", _P), ("stride", _I64 * 3)] + \
+        [(n, _I32) for n in ("n_pages", "page_size", "kv_heads", "head_dim", "dtype", "reserved")]
+
+
 class LayoutParams(ctypes.Structure):
     _fields_ = [(n, _I32) for n in ("n_req", "n_tok", "page_size", "table_width", "n_free",
                                     "first_pos")] + [("flags", _U32), ("reserved", _I32)]
@@ -58,6 +67,16 @@ class AttnParams(ctypes.Structure):
                                     "n_sink", "prefix_len")] + \
         [("scale", _F32), ("flags", _U32), ("q_token_stride", _I64), ("q_head_stride", _I64),
          ("out_token_stride", _I64), ("out_head_stride", _I64)]
+
+
+class ReadParams(ctypes.Structure):
+    _fields_ = [("n_tok", _I32), ("flags", _U32), ("token_stride", _I64), ("head_stride", _I64)]
+
+
+class EvictParams(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("n_req", "table_width", "page_size", "n_sink", "n_recent",
+                                    "n_freed")] + \
+        [("flags", _U32), ("reserved", _I32), ("weight_stride", _I64)]
 
 
 def _current(x):
@@ -148,13 +167,123 @@ def attend_workspace(n_tok: int, n_req: int, q_heads: int, kv_heads: int, head_d
                      window: int = 0, n_sink: int = 0):
     """A workspace (uint8 GPU tensor) for ``attend`` / ``attend_shared`` calls of this
     shape, 256-byte aligned; calls that may overlap in time need one each."""
-    c = KvCache(n_pages=0, page_size=page_size, kv_heads=kv_heads, head_dim=head_dim)
+    return _workspace("fsched_attend_workspace",
+                      KvCache(n_pages=0, page_size=page_size, kv_heads=kv_heads,
+                              head_dim=head_dim),
+                      n_tok, n_req, q_heads, table_width, max_q, prefix_len, window, n_sink)
+
+
+def _workspace(name, c, n_tok, n_req, q_heads, table_width, max_q, prefix_len, window, n_sink):
     p = AttnParams(n_req=n_req, n_tok=n_tok, q_heads=q_heads,
                    max_q=max(1, n_tok) if max_q is None else max_q, table_width=table_width,
                    window=window, n_sink=n_sink, prefix_len=prefix_len, scale=1.0,
                    flags=_fs.F_DEVICE_PTRS)
     size = _I64(0)
-    rc = _fs.lib().fsched_attend_workspace(ctypes.byref(p), ctypes.byref(c), ctypes.byref(size))
+    rc = getattr(_fs.lib(), name)(ctypes.byref(p), ctypes.byref(c), ctypes.byref(size))
     if rc:
-        raise _fs.FschedError(rc, "fsched_attend_workspace")
+        raise _fs.FschedError(rc, name)
     return torch.empty(max(256, size.value), dtype=torch.uint8, device="cuda")
+
+
+def kv4_cache(n_pages: int, kv_heads: int, page_size: int, head_dim: int, *, device="cuda"):
+    """An empty cache of 4 bits an element (its contents are undefined): uint8 [n_pages,
+    kv_heads, page_size / 16, 17 head_dim], keys and values."""
+    if page_size < 16 or page_size % 16:
+        raise ValueError("a cache of 4 bits has pages of 16 tokens and more, a power of two")
+    return torch.empty(n_pages, kv_heads, page_size // 16, 17 * head_dim, dtype=torch.uint8,
+                       device=device)
+
+
+def qk_norm_rope4(qkv, positions, slots, cos_sin, cache, q_weight=None, k_weight=None, *,
+                  eps: float = 1e-6, interleaved: bool = False, out=None, stream=None):
+    """fsched_qk_norm_rope4: ``qk_norm_rope`` with keys and values put into a cache of 4
+    bits."""
+    if stream is not None:
+        with _on(stream, qkv):
+            return qk_norm_rope4(qkv, positions, slots, cos_sin, cache, q_weight, k_weight,
+                                 eps=eps, interleaved=interleaved, out=out)
+    return _step.qk_norm_rope4(qkv, positions, slots, cos_sin, cache, q_weight, k_weight, eps,
+                               interleaved, out, _current(qkv))
+
+
+def kv4_read(cache, slots, *, dtype=torch.bfloat16, stream=None):
+    """fsched_kv4_read: what a cache of 4 bits holds at ``slots`` [n] (-1: zeros), as
+    (keys, values) [n, kv_heads, head_dim] of ``dtype``, the type of the rows that were
+    stored."""
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("dtype must be torch.bfloat16 or torch.float16")
+    if stream is not None:
+        with _on(stream, cache):
+            return kv4_read(cache, slots, dtype=dtype)
+    return _step.kv4_read(cache, slots, dtype == torch.float16, _current(cache))
+
+
+def attend4(q, cache, block_table, q_start, kv_len, *, prefix_pages=None, prefix_len: int = 0,
+            scale=None, window: int = 0, n_sink: int = 0, max_q=None, out=None,
+            return_lse: bool = False, workspace=None, stream=None):
+    """fsched_attend4: ``attend`` (with ``prefix_pages`` and ``prefix_len``:
+    ``attend_shared``) over a cache of 4 bits.  The elements of ``q`` say how the cache's
+    are read.  ``workspace``: of ``attend4_workspace``."""
+    if stream is not None:
+        with _on(stream, q):
+            return attend4(q, cache, block_table, q_start, kv_len, prefix_pages=prefix_pages,
+                           prefix_len=prefix_len, scale=scale, window=window, n_sink=n_sink,
+                           max_q=max_q, out=out, return_lse=return_lse, workspace=workspace)
+    return _step.attend4(q, cache, prefix_pages, prefix_len, block_table, q_start, kv_len, scale,
+                         window, n_sink, max_q, out, return_lse, workspace, _current(q))
+
+
+def attend4_workspace(n_tok: int, n_req: int, q_heads: int, kv_heads: int, head_dim: int, *,
+                      page_size: int, table_width: int, max_q=None, prefix_len: int = 0,
+                      window: int = 0, n_sink: int = 0):
+    """``attend_workspace`` for ``attend4`` calls."""
+    return _workspace("fsched_attend4_workspace",
+                      Kv4Cache(n_pages=0, page_size=page_size, kv_heads=kv_heads,
+                               head_dim=head_dim),
+                      n_tok, n_req, q_heads, table_width, max_q, prefix_len, window, n_sink)
+
+
+def attend_weight(q, lse, k_cache, block_table, q_start, kv_len, weight, *, scale=None,
+                  window: int = 0, n_sink: int = 0, prefix_len: int = 0, max_q=None, stream=None):
+    """fsched_attend_weight: adds to ``weight`` [n_req, width * page_size] (float32, rows
+    may be apart) what each held token gets of the new tokens' attention, summed over
+    tokens and heads.  ``lse`` [n_tok, q_heads] is what ``attend`` of the same arguments
+    returned (``attend_shared`` with ``prefix_len``).  Returns ``weight``."""
+    if stream is not None:
+        with _on(stream, q):
+            return attend_weight(q, lse, k_cache, block_table, q_start, kv_len, weight,
+                                 scale=scale, window=window, n_sink=n_sink,
+                                 prefix_len=prefix_len, max_q=max_q)
+    return _step.attend_weight(q, lse, k_cache, block_table, q_start, kv_len, weight, scale,
+                               window, n_sink, max_q, prefix_len, _current(q))
+
+
+def attend4_weight(q, lse, cache, block_table, q_start, kv_len, weight, *, scale=None,
+                   window: int = 0, n_sink: int = 0, prefix_len: int = 0, max_q=None,
+                   stream=None):
+    """fsched_attend4_weight: ``attend_weight`` over a cache of 4 bits."""
+    if stream is not None:
+        with _on(stream, q):
+            return attend4_weight(q, lse, cache, block_table, q_start, kv_len, weight,
+                                  scale=scale, window=window, n_sink=n_sink,
+                                  prefix_len=prefix_len, max_q=max_q)
+    return _step.attend4_weight(q, lse, cache, block_table, q_start, kv_len, weight, scale,
+                                window, n_sink, max_q, prefix_len, _current(q))
+
+
+def kv_evict(weight, kv_len, block_table, budget, *, page_size: int, n_sink: int = 0,
+             n_recent: int = 0, n_freed=None, stream=None):
+    """fsched_kv_evict: pages of least ``weight`` [n_req, width * page_size] given up until
+    every request holds at most ``budget`` [n_req] tokens, but for its first ``n_sink`` and
+    last ``n_recent``.  ``n_freed``: room for ids of freed pages (None: for the whole
+    table's).
+
+    Returns (block_table, weight, kv_len, freed [n_freed], count [1]), new tensors: tables
+    and weights closed up (behind what stays -1 and 0), the ids of the freed pages with -1
+    behind them, and how many there are."""
+    if stream is not None:
+        with _on(stream, weight):
+            return kv_evict(weight, kv_len, block_table, budget, page_size=page_size,
+                            n_sink=n_sink, n_recent=n_recent, n_freed=n_freed)
+    return _step.kv_evict(weight, kv_len, block_table, budget, page_size, n_sink, n_recent,
+                          n_freed, _current(weight))
