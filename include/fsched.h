@@ -552,6 +552,9 @@ int fsched_attend4_workspace(const fsched_attn_params* p, const fsched_kv4_cache
  *   p               as in the attention call; the strides of out are not used, and with
  *                   prefix_len > 0 the requests' own tokens are meant, behind the prefix,
  *                   whose keys get no weight
+ *                   (at most 2^30 rows of a request and key head, max_q times the group
+ *                   q_heads / kv_heads, and 64 / group + 2 tokens and a group's heads of q
+ *                   within 2^30 elements: ETOOLARGE)
  *   kv              keys only: v may be NULL
  *   lse             [n_tok][q_heads]
  *   weight          in/out [n_req], rows weight_stride elements apart (>= table_width *

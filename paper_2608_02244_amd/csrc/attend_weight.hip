@@ -1,37 +1,90 @@
-// Attention weight of held tokens: launches (attend_weight.hpp).
+// Attention weight of held tokens: which kernels a call runs (attend_weight.hpp).
 #include "attend_weight.hpp"
 
 namespace fs {
 namespace {
 
-template <class T, int D, bool FP4>
-hipError_t launch(const WeightArgs& a, int n_cu, hipStream_t s) {
-  const size_t lds = (size_t)(ATT_WAVES + a.at.n_req + 1) * sizeof(int64_t);
-  weight_rows_kernel<T, D, FP4><<<dim3((unsigned)(2 * n_cu)), ATT_THREADS, lds, s>>>(a);
+// What a call of this shape launches.
+struct Shape {
+  bool few, many;  // requests of either kind are possible
+  WeightPlan plan;
+  size_t bytes;
+};
+
+size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+Shape shape_of(const WeightArgs& a, int head_dim, int n_cu, char* ws) {
+  Shape s;
+  __builtin_memset((void*)&s, 0, sizeof(s));
+  const int64_t most = (int64_t)a.at.max_q * a.at.group;  // rows of one request, at most
+  s.few = a.at.group <= WEIGHT_FEW;
+  s.many = most > WEIGHT_FEW;
+  if (s.many) {
+    const int keys = head_dim == 256 ? WeightTileOf<256>::KEYS : WeightTileOf<128>::KEYS;
+    s.plan.blocks = 2 * n_cu;
+    const size_t parts = round256((size_t)2 * s.plan.blocks * keys * sizeof(float));
+    s.plan.part = (float*)ws;
+    s.plan.tiles = (WeightTile*)(ws ? ws + parts : nullptr);
+    s.bytes = parts + round256((size_t)s.plan.blocks * sizeof(WeightTile));
+  }
+  return s;
+}
+
+template <class T, int D, int KIND>
+hipError_t launch_kind(const WeightArgs& a, const Shape& p, int n_cu, hipStream_t s) {
+  const size_t line = (size_t)(ATT_WAVES + a.at.n_req + 1) * sizeof(int64_t);
+  if (p.few) {
+    const dim3 grid((unsigned)(2 * n_cu));
+    if ((int64_t)a.at.max_q * a.at.group <= 16)
+      weight_rows_kernel<T, D, 1, KIND><<<grid, ATT_THREADS, line, s>>>(a);
+    else
+      weight_rows_kernel<T, D, 2, KIND><<<grid, ATT_THREADS, line, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !p.many) return e;
+  }
+  using L = WeightTileOf<D>;
+  const size_t lds = L::LDS + line;
+  void (*kernel)(WeightArgs, WeightPlan) = weight_tiles_kernel<T, D, KIND>;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(
+        (const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<p.plan.blocks, ATT_THREADS, lds, s>>>(a, p.plan);
+  weight_join_kernel<L::KEYS><<<p.plan.blocks, L::KEYS, 0, s>>>(a, p.plan);
   return hipGetLastError();
 }
 
-template <class T, bool FP4>
-hipError_t launch_dim(const WeightArgs& a, int head_dim, int n_cu, hipStream_t s) {
+template <class T, int D>
+hipError_t launch(const WeightArgs& a, bool fp4, const Shape& p, int n_cu, hipStream_t s) {
+  if (fp4) return launch_kind<T, D, FP4_PAGES>(a, p, n_cu, s);
+  return a.at.kv.page_shift >= WIDE_SHIFT ? launch_kind<T, D, WIDE_PAGES>(a, p, n_cu, s)
+                                          : launch_kind<T, D, SMALL_PAGES>(a, p, n_cu, s);
+}
+
+template <class T>
+hipError_t launch_dim(const WeightArgs& a, bool fp4, int head_dim, const Shape& p, int n_cu,
+                      hipStream_t s) {
   switch (head_dim) {
-    case 64: return launch<T, 64, FP4>(a, n_cu, s);
-    case 128: return launch<T, 128, FP4>(a, n_cu, s);
-    default: return launch<T, 256, FP4>(a, n_cu, s);
+    case 64: return launch<T, 64>(a, fp4, p, n_cu, s);
+    case 128: return launch<T, 128>(a, fp4, p, n_cu, s);
+    default: return launch<T, 256>(a, fp4, p, n_cu, s);
   }
 }
 
 }  // namespace
 
-size_t weight_workspace(const WeightArgs&, bool, int, int) { return 0; }
+size_t weight_workspace(const WeightArgs& a, bool, int head_dim, int n_cu) {
+  return shape_of(a, head_dim, n_cu > 0 ? n_cu : 256, nullptr).bytes;
+}
 
-hipError_t launch_weight(const WeightArgs& a, bool fp4, int dtype, int head_dim, int n_cu, void*,
-                         hipStream_t s) {
+hipError_t launch_weight(const WeightArgs& a, bool fp4, int dtype, int head_dim, int n_cu,
+                         void* workspace, hipStream_t s) {
   if (n_cu <= 0) n_cu = 256;
-  if (dtype == FSCHED_BF16)
-    return fp4 ? launch_dim<Bf16, true>(a, head_dim, n_cu, s)
-               : launch_dim<Bf16, false>(a, head_dim, n_cu, s);
-  return fp4 ? launch_dim<F16, true>(a, head_dim, n_cu, s)
-             : launch_dim<F16, false>(a, head_dim, n_cu, s);
+  if (a.at.kv.n_pages == 0) return hipSuccess;  // no key is held
+  const Shape p = shape_of(a, head_dim, n_cu, (char*)workspace);
+  return dtype == FSCHED_BF16 ? launch_dim<Bf16>(a, fp4, head_dim, p, n_cu, s)
+                              : launch_dim<F16>(a, fp4, head_dim, p, n_cu, s);
 }
 
 }  // namespace fs

@@ -241,6 +241,15 @@ int attend_bytes(const fsched_attn_params* p, const Cache* kv, int64_t* bytes) {
   return FSCHED_OK;
 }
 
+// Rows of a request and key head (its tokens times the query heads) are counted in 32 bits,
+// and 64 of them are addressed by 32-bit offsets from the first one's token.
+bool rows_fit(const fsched_attn_params* p, const AnyCache& c) {
+  const int64_t group = p->q_heads / c.kv_heads;
+  if (p->max_q * group > (1 << 30)) return false;
+  if (p->q_token_stride > kMaxStride || p->q_head_stride > kMaxStride) return false;
+  return (64 / group + 2) * p->q_token_stride + group * p->q_head_stride + c.head_dim <= (1 << 30);
+}
+
 template <class Cache>
 int weight_entry(const fsched_attn_params* p, const Cache* kv, const void* q, const float* lse,
                  const int32_t* table, const int32_t* q_start, const int32_t* kv_len,
@@ -251,6 +260,7 @@ int weight_entry(const fsched_attn_params* p, const Cache* kv, const void* q, co
   if (rc) return rc;
   if (weight_stride < (int64_t)p->table_width * c.page_size) return FSCHED_EINVAL;
   if (weight_stride > kMaxStride) return FSCHED_ETOOLARGE;
+  if (!rows_fit(p, c)) return FSCHED_ETOOLARGE;
   if (p->n_tok == 0 || p->n_req == 0 || p->table_width == 0) return FSCHED_OK;
   if (!q || !lse || !table || !q_start || !kv_len || !weight) return FSCHED_EINVAL;
   if (c.n_pages > 0 && !c.held) return FSCHED_EINVAL;
@@ -261,6 +271,7 @@ int weight_entry(const fsched_attn_params* p, const Cache* kv, const void* q, co
   a.at.table = table;
   a.at.q_start = q_start;
   a.at.kv_len = kv_len;
+  a.group.set(a.at.group);
   a.lse = lse;
   a.weight = weight;
   a.weight_stride = weight_stride;
@@ -282,6 +293,7 @@ int weight_bytes(const fsched_attn_params* p, const Cache* kv, int64_t* bytes) {
   AnyCache c;
   const int rc = check_attn(p, kv, false, &c);
   if (rc) return rc;
+  if (!rows_fit(p, c)) return FSCHED_ETOOLARGE;
   *bytes = 0;
   if (p->n_tok == 0 || p->n_req == 0 || p->table_width == 0) return FSCHED_OK;
   fs::WeightArgs a;

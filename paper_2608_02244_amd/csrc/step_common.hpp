@@ -67,9 +67,26 @@ struct AttnArgs {
   float* lse;  // nullable
 };
 
+// Division of whole numbers below 2^31 by a divisor d that a launch knows:  with
+// 2^l >= d > 2^(l - 1) and m = floor(2^(31 + l) / d) + 1, which fits 32 bits,
+// floor(n / d) = floor(n m / 2^(31 + l)).
+struct Divisor {
+  uint32_t m;
+  int32_t shift;  // l - 1; -1: d is 1
+  void set(int32_t d) {
+    shift = -1;
+    while ((int64_t)1 << (shift + 1) < d) ++shift;
+    m = shift < 0 ? 0 : (uint32_t)(((uint64_t)1 << (32 + shift)) / (uint32_t)d + 1);
+  }
+  __device__ __forceinline__ int divide(int n) const {
+    return shift < 0 ? n : (int)(__umulhi((uint32_t)n, m) >> shift);
+  }
+};
+
 // The attention weight of held tokens: of `at` q, the tables and the cache's keys.
 struct WeightArgs {
   AttnArgs at;
+  Divisor group;
   const float* lse;
   float* weight;
   int64_t weight_stride;
