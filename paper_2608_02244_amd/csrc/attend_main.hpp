@@ -26,7 +26,7 @@ __device__ __forceinline__ void rows_block(const AttnArgs& a, const RowsPlan& p,
 }
 
 template <class T, int D, int RT, int KIND>
-__global__ __launch_bounds__(ATT_THREADS, rows_occupancy(D, KIND == FP4_PAGES)) void
+__global__ __launch_bounds__(ATT_THREADS, rows_occupancy(D, KIND == FP4_PAGES, RT)) void
 attend_rows_kernel(AttnArgs a, MainPlan p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   rows_block<T, D, RT, KIND>(a, p.rows, blockIdx.x, lds);

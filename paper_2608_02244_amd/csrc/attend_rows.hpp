@@ -43,6 +43,7 @@ struct RowsPlan {
   int32_t waves;        // of the launch
   int32_t row_tiles;    // 16-row tiles of a request and key head (1 or 2)
   int32_t slot_rows;    // rows of a part's slot
+  int32_t most_parts;   // of a tile, on average
   int32_t keep_parts;   // 1: results join with those of the prefix, written as parts
   float* part_o;        // [slots][slot_rows][head_dim]; slots: 2 per wave, then with
                         // keep_parts one per tile, for those that lie in one piece
@@ -58,6 +59,9 @@ constexpr int UNIT = 32;       // keys of a unit
 //    65,536 tokens, 1 key head    436 / 119 /  49 /  42 us
 //     4,096 tokens, 1 key head     35 /  17 /  18 /  18 us
 constexpr int MOST_PARTS = 128;
+// Over a cache of 4 bits, whose units take less time, two requests of 95,000 tokens and 8 key
+// heads: 57 us with 128, 55 with 256 (that is all waves there).
+constexpr int MOST_PARTS4 = 256;
 
 // Blocks per compute unit.  Fewer waves have longer pieces, more of them more loads under
 // way.  The registers would allow 4 with heads of 64 and 3 with heads of 128 (one row tile,
@@ -69,8 +73,11 @@ constexpr int MOST_PARTS = 128;
 //                  64 requests                                  - /  35 /  35 /  36
 //   heads of 256   64 requests, pages of 16 and of 8          108 / 117, 107 / 126
 //                  64 drafts; one request of 131,072 tokens   122 / 136, 218 / 211
-constexpr int rows_occupancy(int D, bool fp4) {
-  return fp4 ? (D == 256 ? 2 : 3) : D == 64 ? 3 : D == 128 ? 2 : 1;
+// Over a cache of 4 bits, whose loads are shorter, as many as the registers leave (a second
+// row tile takes one place of heads of 64 and 128).
+constexpr int rows_occupancy(int D, bool fp4, int row_tiles) {
+  if (fp4) return D == 256 ? 2 : (D == 64 ? 4 : 3) - (row_tiles == 2);
+  return D == 64 ? 3 : D == 128 ? 2 : 1;
 }
 
 // The line of units and a wave's piece of it.
@@ -141,7 +148,8 @@ __device__ __forceinline__ RowsLine rows_line(const AttnArgs& a, const RowsPlan&
   l.total = l.per_head * a.kv.kv_heads;
   // Waves with work: a few tiles are not cut finer than their parts are worth reading
   // again.  Wave i takes units i total / waves .. (i + 1) total / waves.
-  l.waves = min(min((int64_t)plan.waves, l.total), (int64_t)MOST_PARTS * a.n_req * a.kv.kv_heads);
+  l.waves = min(min((int64_t)plan.waves, l.total),
+                (int64_t)plan.most_parts * a.n_req * a.kv.kv_heads);
   l.me = uni_int(block * ATT_WAVES + wave);
   l.begin = l.end = 0;
   if (l.me < l.waves) {

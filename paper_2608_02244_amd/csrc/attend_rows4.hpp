@@ -109,17 +109,18 @@ __device__ __forceinline__ void attend_rows4(const AttnArgs& a, const RowsPlan& 
       const int s0 = sp.block(u) * UNIT;
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const bool held = (uint32_t)pages[b] < (uint32_t)a.kv.n_pages;
+        const int at = uni_int(pages[b]);
+        const bool held = (uint32_t)at < (uint32_t)a.kv.n_pages;
         y.found |= held ? seen(s0 + b * GROUP) << (b * 16) : 0;
         // a group that is not there reads page 0, which exists if any group does
-        const uint32_t page = held ? pages[b] : 0;
+        const uint32_t page = held ? at : 0;
         const uint32_t slot = (uint32_t)(s0 + b * GROUP) & page_mask;
         const char* g = base + page * (uint64_t)a.kv.k_page +
                         (slot >> GROUP_SHIFT) * (uint64_t)a.kv.k_slot;
 #pragma unroll
         for (int i = 0; i < Unit::WORDS; ++i) {
-          y.k[b][i] = ((const uint32_t*)(g + k_lane))[i];
-          y.v[b][i] = ((const uint32_t*)(g + v_lane))[i];
+          y.k[b][i] = __builtin_nontemporal_load((const uint32_t*)(g + k_lane) + i);
+          y.v[b][i] = __builtin_nontemporal_load((const uint32_t*)(g + v_lane) + i);
         }
         y.k_scale[b] = D == 256 ? *(const uint16_t*)(g + ks_lane) : *(const uint8_t*)(g + ks_lane);
         y.v_scale[b] = *(const uint32_t*)(g + vs_lane);
@@ -127,31 +128,10 @@ __device__ __forceinline__ void attend_rows4(const AttnArgs& a, const RowsPlan& 
       return y;
     };
 
-    // units u0 .. last: pages are looked up two ahead, loads are one ahead
-    const int last = sp.blocks > 0 && a.kv.n_pages > 0 ? u1 : u0;
-    Unit next;
-    int pages[2] = {-1, -1};
-    if (last > u0) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b) pages[b] = page_of(u0, b);
-      next = load(u0, pages);
-      if (u0 + 1 < last) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) pages[b] = page_of(u0 + 1, b);
-      }
-    }
-    for (int u = u0; u < last; ++u) {
+    auto work = [&](int u, const Unit& y) {
       const int s0 = sp.block(u) * UNIT;
-      const Unit y = next;
-      if (u + 1 < last) {
-        next = load(u + 1, pages);
-        if (u + 2 < last) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b) pages[b] = page_of(u + 2, b);
-        }
-      }
       const uint32_t found = y.found;
-      if (found == 0) continue;
+      if (found == 0) return;
       // all 32 keys held, and seen by every row
       const bool full = found == ~0u && s0 + UNIT - 1 <= first_own &&
                         (a.window == 0 || s0 > last_own - a.window || s0 + UNIT <= sink_keys);
@@ -164,6 +144,7 @@ __device__ __forceinline__ void attend_rows4(const AttnArgs& a, const RowsPlan& 
           const uint32_t byte = D == 256 ? (y.k_scale[b] >> (c / 4 * 8)) & 255 : y.k_scale[b];
           k[b][c] = __builtin_bit_cast(x8, values8<T>(y.k[b][c], scale_of(byte)));
         }
+      const uint32_t mine = found >> (4 * h);  // bits of the lane's keys
       x8 p[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
@@ -180,9 +161,9 @@ __device__ __forceinline__ void attend_rows4(const AttnArgs& a, const RowsPlan& 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int key = s0 + b * 16 + 4 * h + i;
-              const bool see = ((found >> (b * 16 + 4 * h + i)) & 1) && key <= top[t] &&
-                               (key > low[t] || key < sink_keys);
-              if (!see) s[b][i] = NEG_INF;
+              const bool see = (bool)((mine >> (b * 16 + i)) & 1) & (key <= top[t]) &
+                               ((key > low[t]) | (key < sink_keys));
+              s[b][i] = see ? s[b][i] : NEG_INF;
             }
         }
         float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
@@ -206,14 +187,19 @@ __device__ __forceinline__ void attend_rows4(const AttnArgs& a, const RowsPlan& 
         }
       }
 
+      uint32_t v_scale[2] = {y.v_scale[0], y.v_scale[1]};
+      if (found != ~0u) {
+        // where no key is the scale may be NaN, and 0 * NaN is NaN
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!((mine >> (b * 16 + i)) & 1))
+              v_scale[b] = (v_scale[b] & ~(255u << (8 * i))) | 127u << (8 * i);
+      }
       float vs[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        uint32_t byte = (y.v_scale[j >> 2] >> (8 * (j & 3))) & 255;
-        // where no key is the scale may be NaN, and 0 * NaN is NaN
-        if (found != ~0u && !((found >> ((j & 3) + 4 * h + (j >> 2) * 16)) & 1)) byte = 127;
-        vs[j] = scale_of(byte);
-      }
+      for (int j = 0; j < 8; ++j) vs[j] = scale_of((v_scale[j >> 2] >> (8 * (j & 3))) & 255);
       auto values = [&](auto at) {  // elements 2i and 2i + 1 of the lane's 8 keys
         constexpr int i = decltype(at)::value;
         uint32_t z[8];
@@ -239,6 +225,34 @@ __device__ __forceinline__ void attend_rows4(const AttnArgs& a, const RowsPlan& 
         }
       };
       each<DL / 2>(values);
+    };
+
+    // units u0 .. last, two in turn: while one is worked on the next one's loads are under
+    // way, and its own place is loaded again behind it.  Pages are looked up before that.
+    const int last = sp.blocks > 0 && a.kv.n_pages > 0 ? u1 : u0;
+    Unit ready[2];
+    int pages[2] = {-1, -1};
+    auto look_up = [&](int u) {
+      if (u < last) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) pages[b] = page_of(u, b);
+      }
+    };
+    look_up(u0);
+    if (u0 < last) ready[0] = load(u0, pages);
+    look_up(u0 + 1);
+    if (u0 + 1 < last) ready[1] = load(u0 + 1, pages);
+    look_up(u0 + 2);
+    for (int u = u0; u < last; u += 2) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (u + i >= last) break;
+        work(u + i, ready[i]);
+        if (u + i + 2 < last) {
+          ready[i] = load(u + i + 2, pages);
+          look_up(u + i + 3);
+        }
+      }
     }
     rows_write<T, D, RT>(a, plan, line, part, w, x, rows, o, mu, l);
     w += u1 - u0;

@@ -13,12 +13,15 @@ struct Shape {
 
 size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 
+int64_t most_rows(const WeightArgs& a) {  // of one request and key head
+  return (int64_t)a.at.max_q * a.at.group;
+}
+
 Shape shape_of(const WeightArgs& a, int head_dim, int n_cu, char* ws) {
   Shape s;
   __builtin_memset((void*)&s, 0, sizeof(s));
-  const int64_t most = (int64_t)a.at.max_q * a.at.group;  // rows of one request, at most
   s.few = a.at.group <= WEIGHT_FEW;
-  s.many = most > WEIGHT_FEW;
+  s.many = most_rows(a) > WEIGHT_FEW;
   if (s.many) {
     const int keys = head_dim == 256 ? WeightTileOf<256>::KEYS : WeightTileOf<128>::KEYS;
     s.plan.blocks = 2 * n_cu;
@@ -34,11 +37,13 @@ template <class T, int D, int KIND>
 hipError_t launch_kind(const WeightArgs& a, const Shape& p, int n_cu, hipStream_t s) {
   const size_t line = (size_t)(ATT_WAVES + a.at.n_req + 1) * sizeof(int64_t);
   if (p.few) {
-    const dim3 grid((unsigned)(2 * n_cu));
-    if ((int64_t)a.at.max_q * a.at.group <= 16)
-      weight_rows_kernel<T, D, 1, KIND><<<grid, ATT_THREADS, line, s>>>(a);
+    constexpr bool FP4 = KIND == FP4_PAGES;
+    if (most_rows(a) <= 16)
+      weight_rows_kernel<T, D, 1, KIND>
+          <<<(unsigned)(weight_occupancy(D, 1, FP4) * n_cu), ATT_THREADS, line, s>>>(a);
     else
-      weight_rows_kernel<T, D, 2, KIND><<<grid, ATT_THREADS, line, s>>>(a);
+      weight_rows_kernel<T, D, 2, KIND>
+          <<<(unsigned)(weight_occupancy(D, 2, FP4) * n_cu), ATT_THREADS, line, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !p.many) return e;
   }
