@@ -97,11 +97,20 @@ __device__ __forceinline__ u32x4 values8(uint32_t codes, float scale) {
 // A 64-bit number to 32 bits so that rounding it again to fewer bits gives what rounding the
 // number itself gives: towards zero, the last bit set where something was cut off.
 __device__ __forceinline__ float to_odd(double x) {
-  const float f = (float)x;
-  uint32_t b = __builtin_bit_cast(uint32_t, f);
-  if (fabs((double)f) > fabs(x)) --b;
-  if ((double)__builtin_bit_cast(float, b) != x) b |= 1;
-  return __builtin_bit_cast(float, b);
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t hi = (uint32_t)(b >> 32), lo = (uint32_t)b;
+  const uint32_t e = (hi >> 20) & 0x7ff;
+  uint32_t r;
+  if (e - 897u < 254u) {  // a normal number of 32 bits: exponent and mantissa from the 64
+    r = (hi & 0x80000000u) | (((hi & 0x7fffffffu) << 3 | lo >> 29) - (896u << 23));
+    r |= (lo & 0x1fffffffu) != 0;
+  } else {
+    const float f = (float)x;
+    r = __builtin_bit_cast(uint32_t, f);
+    if (fabs((double)f) > fabs(x)) --r;
+    if ((double)__builtin_bit_cast(float, r) != x) r |= 1;
+  }
+  return __builtin_bit_cast(float, r);
 }
 
 }  // namespace fs
