@@ -84,7 +84,8 @@ __device__ __forceinline__ void exact_key(typename T::x8 raw, const void* weight
 
 // FP4: the cache holds 4 bits an element; its strides are bytes, k_slot that of a group.
 template <class T, int D, bool INTER, bool FP4>
-__global__ __launch_bounds__(THREADS, FP4 ? 6 : 1) void qk_rope_kernel(RopeArgs a, int chunks, int per_chunk) {
+__global__ __launch_bounds__(THREADS, FP4 ? 6 : 1) void qk_rope_kernel(RopeArgs a, int chunks,
+                                                                      int per_chunk) {
   constexpr int LANES = D / 8;        // lanes of one head vector
   constexpr int HEADS = 64 / LANES;   // head vectors a wave holds at once
   using x8 = typename T::x8;
@@ -136,61 +137,66 @@ __global__ __launch_bounds__(THREADS, FP4 ? 6 : 1) void qk_rope_kernel(RopeArgs 
 
   const elem* in = (const elem*)a.qkv + t * a.qkv_stride + d0;
   x8 next = {};
-  if (FP4 && h0 + grp < h1) next = __builtin_nontemporal_load((const x8*)(in + (int64_t)(h0 + grp) * D));
+  auto head_at = [&](int h) {
+    return __builtin_nontemporal_load((const x8*)(in + (int64_t)h * D));
+  };
+  if (FP4 && h0 + grp < h1) next = head_at(h0 + grp);
   for (int h = h0 + grp; h - grp < h1; h += HEADS) {
     const bool on = h < h1;  // lanes past the last head help their wave's exchanges
     x8 raw = {};
     if constexpr (FP4) {  // the heads' work is uneven, so the next ones are under way
       raw = next;
-      if (h + HEADS < h1) next = __builtin_nontemporal_load((const x8*)(in + (int64_t)(h + HEADS) * D));
+      if (h + HEADS < h1) next = head_at(h + HEADS);
     } else {
-      if (on) raw = __builtin_nontemporal_load((const x8*)(in + (int64_t)h * D));
+      if (on) raw = head_at(h);
     }
     const bool is_q = h < a.q_heads, is_k = !is_q && h < a.q_heads + a.kv.kv_heads;
     float x[8];
     const void* weight = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
-    if (!FP4 || is_q) {  // keys and values of a cache of 4 bits: below
-      float sq = 0.0f;
+    float sq = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] = (float)raw[i];
-        sq = fmaf(x[i], x[i], sq);
-      }
+    for (int i = 0; i < 8; ++i) {
+      x[i] = (float)raw[i];
+      sq = fmaf(x[i], x[i], sq);
+    }
 #pragma unroll
-      for (int d = 1; d < LANES; d <<= 1) sq += __shfl_xor(sq, d);
-      if (weight) {
-        const float r = 1.0f / sqrtf(sq * (1.0f / D) + a.eps);
-        const x8 g = *(const x8*)((const elem*)weight + d0);
+    for (int d = 1; d < LANES; d <<= 1) sq += __shfl_xor(sq, d);
+    if (weight) {
+      const float r = 1.0f / sqrtf(sq * (1.0f / D) + a.eps);
+      const x8 g = *(const x8*)((const elem*)weight + d0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (float)g[i];
-      }
-      if (a.rot_dim > 0) {
-        if (INTER) {
-          if (rotated && known && (is_q || is_k)) {
+      for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (float)g[i];
+    }
+    if (a.rot_dim > 0) {
+      if (INTER) {
+        if (rotated && known && (is_q || is_k)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float p = x[2 * i], q = x[2 * i + 1];
+          for (int i = 0; i < 4; ++i) {
+            const float p = x[2 * i], q = x[2 * i + 1];
+            if constexpr (FP4) {  // rounded as the compiler's choice for the other is
+              x[2 * i] = fmaf(p, c[i], -(q * s[i]));
+              x[2 * i + 1] = fmaf(p, s[i], q * c[i]);
+            } else {
               x[2 * i] = p * c[i] - q * s[i];
               x[2 * i + 1] = q * c[i] + p * s[i];
             }
           }
-        } else {
-          float y[8];
+        }
+      } else {
+        float y[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = __shfl(x[i], partner & 63);
-          if (rotated && known && (is_q || is_k)) {
+        for (int i = 0; i < 8; ++i) y[i] = __shfl(x[i], partner & 63);
+        if (rotated && known && (is_q || is_k)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] * c[i] + y[i] * s[i];
-          }
+          for (int i = 0; i < 8; ++i)
+            x[i] = FP4 ? fmaf(x[i], c[i], y[i] * s[i]) : x[i] * c[i] + y[i] * s[i];
         }
       }
     }
     if (!on) continue;
-    x8 res = {};
-    if (!FP4 || is_q) {
+    x8 res;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) res[i] = (elem)x[i];
-    }
+    for (int i = 0; i < 8; ++i) res[i] = (elem)x[i];
     if (is_q) {
       const x8 zero = {};
       *(x8*)((elem*)a.q_out + t * a.q_token + (int64_t)h * a.q_head + d0) = known ? res : zero;
