@@ -7,6 +7,10 @@ reading: prompt tokens and output tokens alike).  ``Worker`` keeps what a servin
 keeps between steps (the paged cache of every layer, the block table, the free pages, the
 lengths) and runs a step: ``kv_layout`` once, then ``qk_norm_rope`` and ``attend`` per
 layer.  ``play`` drives it through a schedule.
+
+A worker whose memory is the limit holds its cache in 4 bits (``kv_bits=4``), or keeps each
+request within a budget of tokens: the attention weight of held tokens is added up over
+steps and layers, and pages of least weight are given back (``budget``).
 """
 from __future__ import annotations
 
@@ -21,18 +25,34 @@ class Worker:
     """A paged KV cache of ``layers`` layers and the requests that hold parts of it.
 
     Lengths are known on the host (they follow from the schedule), so which pages are free
-    is too; the page ids themselves stay on the GPU."""
+    is too; the page ids themselves stay on the GPU.
+
+    ``kv_bits`` 4: the cache holds 4 bits an element (pages of 16 tokens and more).
+    ``budget``: tokens that a request may keep behind a step.  One that holds more gives up
+    whole pages, those of least attention weight first, but for its first ``n_sink`` and
+    last ``n_recent`` tokens (``kv_evict``); what it keeps stays at its positions, and a
+    window counts kept tokens."""
 
     def __init__(self, *, n_pages: int, page_size: int, q_heads: int, kv_heads: int,
                  head_dim: int, max_len: int, layers: int = 1, rope_base: float = 10000.0,
-                 window: int = 0, n_sink: int = 0, dtype=torch.bfloat16, device="cuda"):
+                 window: int = 0, n_sink: int = 0, dtype=torch.bfloat16, device="cuda",
+                 kv_bits: int = 16, budget=None, n_recent: int = 0):
+        if kv_bits not in (4, 16):
+            raise ValueError("a cache holds 4 or 16 bits an element")
+        if budget is not None and budget < 1:
+            raise ValueError("a budget is at least one token")
         self.page_size, self.q_heads, self.window, self.n_sink = (page_size, q_heads, window,
                                                                   n_sink)
         self.max_len = max_len  # rows of the rotation table; the block table's are whole pages
         self.width = -(-max_len // page_size)
-        self.caches = [tuple(torch.zeros(n_pages, kv_heads, page_size, head_dim, dtype=dtype,
-                                         device=device) for _ in range(2))
-                       for _ in range(layers)]
+        self.kv_bits, self.budget, self.n_recent = kv_bits, budget, n_recent
+        if kv_bits == 4:  # one tensor for keys and values
+            self.caches = [(fs.kv4_cache(n_pages, kv_heads, page_size, head_dim,
+                                         device=device).zero_(),) for _ in range(layers)]
+        else:
+            self.caches = [tuple(torch.zeros(n_pages, kv_heads, page_size, head_dim, dtype=dtype,
+                                             device=device) for _ in range(2))
+                           for _ in range(layers)]
         half = head_dim // 2
         angle = torch.arange(max_len, device=device, dtype=torch.float64)[:, None] * \
             rope_base ** (-torch.arange(half, device=device, dtype=torch.float64) / half)
@@ -41,7 +61,11 @@ class Worker:
         self.free = torch.arange(n_pages, dtype=torch.int32, device=device)
         self.requests: list = []                      # ids, one per row of the table
         self.held: dict = {}                          # tokens of each
+        self.gone: dict = {}                          # tokens of each given up
         self.table = torch.empty(0, self.width, dtype=torch.int32, device=device)
+        # attention weight of held tokens, one row per row of the table
+        self.attention = None if budget is None else \
+            torch.empty(0, self.width * page_size, device=device)
 
     def _pages(self, tokens: int) -> int:
         return -(-tokens // self.page_size)
@@ -57,10 +81,13 @@ class Worker:
                 for i, r in enumerate(self.requests) if r in gone]
         keep = [i for i, r in enumerate(self.requests) if r not in gone]
         self.free = torch.cat([self.free] + back)
-        self.table = self.table[torch.tensor(keep, dtype=torch.long, device=self.table.device)]
+        rows = torch.tensor(keep, dtype=torch.long, device=self.table.device)
+        self.table = self.table[rows]
+        if self.attention is not None:
+            self.attention = self.attention[rows]
         self.requests = [self.requests[i] for i in keep]
         for r in gone:
-            del self.held[r]
+            del self.held[r], self.gone[r]
 
     def admit(self, ids) -> None:
         """Requests that hold nothing yet get a row."""
@@ -71,15 +98,31 @@ class Worker:
             raise ValueError("a request has one row only")
         fresh = self.table.new_full((len(ids), self.width), -1)
         self.table = torch.cat((self.table, fresh))
+        if self.attention is not None:
+            zeros = self.attention.new_zeros(len(ids), self.attention.shape[1])
+            self.attention = torch.cat((self.attention, zeros))
         self.requests += ids
         self.held.update((r, 0) for r in ids)
+        self.gone.update((r, 0) for r in ids)
+
+    def position(self, r) -> int:
+        """Where the next token of request ``r`` sits."""
+        return self.held[r] + self.gone[r]
+
+    def _given_up(self, held: int) -> int:
+        """Pages that a request of so many tokens gives up, as ``kv_evict`` counts them."""
+        over = self._pages(max(0, held - self.budget))
+        first = min(self._pages(self.n_sink), self._pages(held))
+        last = max(0, held - self.n_recent) // self.page_size
+        return min(over, max(0, last - first))
 
     def step(self, new: Sequence[int], qkv: Callable):
         """One step: ``new[i]`` tokens of request ``self.requests[i]``.  ``qkv(layer)`` gives
         the fused projection [sum(new), q_heads + 2 kv_heads, head_dim] of a layer.  Returns
         every layer's attention output."""
         old = [self.held[r] for r in self.requests]
-        if any(o + n > self.max_len for o, n in zip(old, new)):
+        gone = [self.gone[r] for r in self.requests]
+        if any(o + g + n > self.max_len for o, g, n in zip(old, gone, new)):
             raise ValueError("a request outgrows max_len")
         need = sum(self._pages(o + n) - self._pages(o) for o, n in zip(old, new))
         if need > len(self.free):
@@ -89,16 +132,39 @@ class Worker:
         slots, pos, q_start, kv_len, _ = fs.kv_layout(
             lengths[0], lengths[1], self.table, self.free, page_size=self.page_size,
             n_tok=sum(new))
+        if any(gone):  # a token's position counts those before it that were given up
+            pos = pos + torch.tensor([g for g, n in zip(gone, new) for _ in range(n)],
+                                     dtype=torch.int32, device=dev)
+        four = self.kv_bits == 4
+        store, attend = (fs.qk_norm_rope4, fs.attend4) if four else (fs.qk_norm_rope, fs.attend)
+        kw = dict(window=self.window, n_sink=self.n_sink, max_q=max([1, *new]))
+        weight = None if self.attention is None else self.attention.clone()
         out = []
-        for layer, (k, v) in enumerate(self.caches):
-            q = fs.qk_norm_rope(qkv(layer), pos, slots, self.cos_sin, k, v, self.weight,
-                                self.weight)
-            out.append(fs.attend(q, k, v, self.table, q_start, kv_len, window=self.window,
-                                 n_sink=self.n_sink, max_q=max([1, *new])))
+        for layer, cache in enumerate(self.caches):
+            q = store(qkv(layer), pos, slots, self.cos_sin, *cache, self.weight, self.weight)
+            if weight is None:
+                out.append(attend(q, *cache, self.table, q_start, kv_len, **kw))
+                continue
+            y, lse = attend(q, *cache, self.table, q_start, kv_len, return_lse=True, **kw)
+            (fs.attend4_weight if four else fs.attend_weight)(
+                q, lse, cache[0], self.table, q_start, kv_len, weight, **kw)
+            out.append(y)
         # only now: a step that ends with an error (in ``qkv``, say) can be run again
         self.free = self.free[need:]
-        for r, o, n in zip(self.requests, old, new):
-            self.held[r] = o + n
+        held = [o + n for o, n in zip(old, new)]
+        if weight is not None:
+            self.attention = weight
+            up = [self._given_up(m) for m in held]
+            if any(up):
+                self.table, self.attention, _, freed, _ = fs.kv_evict(
+                    weight, kv_len, self.table, torch.full_like(kv_len, self.budget),
+                    page_size=self.page_size, n_sink=self.n_sink, n_recent=self.n_recent,
+                    n_freed=sum(up))
+                self.free = torch.cat((self.free, freed))
+                held = [m - u * self.page_size for m, u in zip(held, up)]
+                for r, u in zip(self.requests, up):
+                    self.gone[r] += u * self.page_size
+        self.held.update(zip(self.requests, held))
         return out
 
 
@@ -126,7 +192,7 @@ def play(worker: Worker, start, finish, qkv: Callable, on_step: Callable = None,
         if not worker.requests:
             continue
         now = list(worker.requests)
-        at = [worker.held[r] for r in now]
+        at = [worker.position(r) for r in now]
         out = worker.step([1] * len(now), lambda layer: qkv(layer, now, at))
         steps += 1
         if on_step:

@@ -667,3 +667,78 @@ def test_step_within_a_budget_in_a_captured_graph(dev):
         b = one()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("budget", [None, 32])
+def test_replay_of_a_schedule(dev, bits, budget):
+    """An ISJL schedule played on a worker with a cache of 4 bits, a budget of tokens, or
+    both.  Which pages a request gave up is read from its row of the table; every token
+    attends over exactly the tokens that its request holds then, at their own positions.
+    The reference has queries in 64 bits, and keys too with 16 bits; rounding them to f16
+    moves a score by at most d = (2 u + u^2) scale sum |q k| (u scale sum |q k| with 4 bits,
+    whose keys are the cache's), and the output by (exp(2 d) - 1) A beside its own rounding."""
+    import numpy as np
+    import torch
+    from paper_2608_02244_amd import replay
+    rng = np.random.default_rng(5)
+    n, Hq, Hkv, D, page, layers, u = 8, 4, 2, 64, 16, 2, U["f16"]
+    a, p, o = (rng.integers(lo, hi, (1, n)).astype(np.int32)
+               for lo, hi in ((0, 20), (1, 90), (1, 60)))
+    _, start, finish = fs.simulate(a, p, o, policy="isjl", B=4, alpha=8, M_kv=600, cost_c=0,
+                                   cost_tau=0, schedule=True)
+    length = (p + o)[0].tolist()
+    g = torch.Generator().manual_seed(9)
+    x = torch.randn(layers, n, max(length), Hq + 2 * Hkv, D, generator=g).half()
+    xd = x.to(dev)
+    w = replay.Worker(n_pages=600 // page + n, page_size=page, q_heads=Hq, kv_heads=Hkv,
+                      head_dim=D, max_len=max(length), layers=layers, dtype=torch.float16,
+                      device=dev, kv_bits=bits, budget=budget, n_recent=8, n_sink=3)
+    pages = len(w.free)
+    y = x.double()
+    y[..., :Hq + Hkv, :] /= (y[..., :Hq + Hkv, :].square().mean(-1, keepdim=True) + 1e-6).sqrt()
+    cs = w.cos_sin.double().cpu()[:max(length), None, :]
+    c, s = cs[..., :D // 2], cs[..., D // 2:]
+    f, e = y[..., :Hq + Hkv, :D // 2].clone(), y[..., :Hq + Hkv, D // 2:].clone()
+    y[..., :Hq + Hkv, :D // 2], y[..., :Hq + Hkv, D // 2:] = f * c - e * s, e * c + f * s
+    if bits == 4:
+        y[..., Hq:, :] = values(*quantise(y[..., Hq:, :], "f16"))
+    holds, rows, seen, given = {}, {}, [0] * n, 0
+    at_step = []
+
+    def on_step(t, now, outs):
+        nonlocal given
+        at_step.append(t)
+        for i, r in enumerate(now):
+            mine = holds.setdefault(r, []) + [seen[r]]  # positions held while it attended
+            seen[r] += 1
+            for layer, out in enumerate(outs):
+                z = y[layer, r]
+                for h in range(Hq):
+                    q, k = z[mine[-1], h], z[mine, Hq + h // 2]
+                    v = z[mine, Hq + Hkv + h // 2]
+                    wt = torch.softmax(k @ q * D ** -0.5, 0)
+                    A = wt @ v.abs()
+                    m = u if bits == 4 else 2 * u + u * u
+                    d = m * D ** -0.5 * float((k.abs() @ q.abs()).max())
+                    tol = math.expm1(2 * d) * A + 1.1 * u * (A + (wt @ v).abs()) + 2.0 ** -18 * (1 + A)
+                    assert ((out[i, h].double().cpu() - wt @ v).abs() <= tol).all()
+            row = w.table[w.requests.index(r)].tolist()
+            before = rows.get(r, [])
+            have = -(-len(mine) // page)
+            kept = [q for q in before[:have] if q in row] if budget else before[:have]
+            if budget and len(kept) < len(before):
+                gone = [j for j, q in enumerate(before) if q not in row]
+                given += len(gone)
+                mine = [x for j, x in enumerate(mine) if j // page not in gone]
+            holds[r] = mine
+            rows[r] = row[:-(-len(mine) // page)]
+            assert w.held[r] == len(mine) and w.position(r) == seen[r]
+        free = w.free.tolist() + [q for r in w.requests for q in rows[r]]
+        assert sorted(free) == list(range(pages))
+    log(f"replay bits={bits} budget={budget} {sum(length)} tokens")
+    replay.play(w, start[0], finish[0],
+                lambda layer, now, at: torch.stack([xd[layer, r, i] for r, i in zip(now, at)]),
+                on_step)
+    assert seen == length and sorted(w.free.tolist()) == list(range(pages))
+    assert bool(given) == bool(budget)
