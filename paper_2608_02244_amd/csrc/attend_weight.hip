@@ -56,6 +56,8 @@ hipError_t launch_kind(const WeightArgs& a, const Shape& p, int n_cu, hipStream_
     if (e != hipSuccess) return e;
   }
   kernel<<<p.plan.blocks, ATT_THREADS, lds, s>>>(a, p.plan);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;  // the join would read what was not written
   weight_join_kernel<L::KEYS><<<p.plan.blocks, L::KEYS, 0, s>>>(a, p.plan);
   return hipGetLastError();
 }

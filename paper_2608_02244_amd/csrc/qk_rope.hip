@@ -153,21 +153,25 @@ __global__ __launch_bounds__(THREADS, FP4 ? 6 : 1) void qk_rope_kernel(RopeArgs 
     const bool is_q = h < a.q_heads, is_k = !is_q && h < a.q_heads + a.kv.kv_heads;
     float x[8];
     const void* weight = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
+    // keys and values of a cache of 4 bits: below
+    const bool here = !FP4 || __ballot(is_q) != 0;
     float sq = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       x[i] = (float)raw[i];
       sq = fmaf(x[i], x[i], sq);
     }
+    if (here) {
 #pragma unroll
-    for (int d = 1; d < LANES; d <<= 1) sq += __shfl_xor(sq, d);
-    if (weight) {
+      for (int d = 1; d < LANES; d <<= 1) sq += __shfl_xor(sq, d);
+    }
+    if (here && weight) {
       const float r = 1.0f / sqrtf(sq * (1.0f / D) + a.eps);
       const x8 g = *(const x8*)((const elem*)weight + d0);
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = x[i] * r * (float)g[i];
     }
-    if (a.rot_dim > 0) {
+    if (here && a.rot_dim > 0) {
       if (INTER) {
         if (rotated && known && (is_q || is_k)) {
 #pragma unroll
