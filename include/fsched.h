@@ -534,6 +534,8 @@ int fsched_kv4_read(const fsched_read_params* p, const fsched_kv4_cache* kv,
 
 /* fsched_attend4 — fsched_attend (prefix_len 0) and fsched_attend_shared over a cache of 4
  * bits: the same arguments, masks and results for the values that the codes stand for.
+ * (Of these, values that are not finite also reach rows of their request that do not see
+ * them, as 0 times NaN; keys do not.)
  * prefix_pages is read only when prefix_len > 0. */
 int fsched_attend4(const fsched_attn_params* p, const fsched_kv4_cache* kv, const void* q,
                    const int32_t* prefix_pages, const int32_t* table, const int32_t* q_start,
@@ -548,7 +550,9 @@ int fsched_attend4_workspace(const fsched_attn_params* p, const fsched_kv4_cache
  *   weight[r][j] += sum of exp(scale q.k_j - lse)
  * over the new tokens of request r and the query heads that see key j, each with its row
  * of lse, as the attention call of the same arguments returned it (a row whose lse is
- * -infinity adds nothing).  Summed over steps and layers it says which tokens are used.
+ * -infinity adds nothing, whatever its q holds; one whose lse is NaN adds NaN to the keys
+ * that it sees and nothing to others).  Summed over steps and layers it says which tokens
+ * are used.
  *   p               as in the attention call; the strides of out are not used, and with
  *                   prefix_len > 0 the requests' own tokens are meant, behind the prefix,
  *                   whose keys get no weight
@@ -589,6 +593,7 @@ int fsched_attend4_weight_workspace(const fsched_attn_params* p, const fsched_kv
  * all come before the last n_recent; those with the least sum of their tokens' weights (in
  * 64 bits) go, of equal ones the earlier.
  *   n_req, table_width, page_size   as elsewhere (page_size any power of two <= 65536)
+ *                   n_req * table_width below 2^31 (ETOOLARGE)
  *   n_sink, n_recent  first and last tokens that stay, >= 0
  *   n_freed         capacity of freed
  *   weight_stride   elements between rows of weight, >= table_width * page_size

@@ -295,7 +295,8 @@ weight_rows_kernel(WeightArgs wa) {
         for (int t = 0; t < RT; ++t) {
           // a row that sees nothing, or is none, gives nothing
           const float l = mine_now.lse[t];
-          const float off = on[t] && l != NEG_INF ? l * LOG2E : -NEG_INF;
+          const bool some = on[t] && l != NEG_INF;
+          const float off = l * LOG2E;
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             f32x4 s = {0, 0, 0, 0};
@@ -305,7 +306,8 @@ weight_rows_kernel(WeightArgs wa) {
             for (int e = 0; e < 4; ++e) {
               const float p = exp2_fast(fmaf(s[e], a.scale_log2, -off));
               const int key = s0 + b * 16 + 4 * h + e;
-              const bool see = full || (key <= top[t] && (key > low[t] || key < sink_keys));
+              const bool see =
+                  some && (full || (key <= top[t] && (key > low[t] || key < sink_keys)));
               sum[b][e] += see ? p : 0.0f;
             }
           }
@@ -618,14 +620,21 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void weight_tiles_kernel(WeightArgs
           asm volatile("" : "+v"(y));
           k[n][c] = __builtin_bit_cast(x8, y);
         }
-      struct Rows {  // of a row tile: the lane's offset and last key; the first and last of all
+      // Of a row tile: the lane's offset and last key, and whether its lse is NaN; the least
+      // of all lanes' keys (-1: some lane is to be looked at) and the greatest.
+      struct Rows {
         float off;
         int last, k0, k1;
+        bool nan;
       };
       auto hide = [&](f32x16& x, int n, const Rows& y) {  // scores of keys that the row does not see
         if (group_key[n] + 31 <= y.k0 && (a.window == 0 || group_key[n] > y.k1 - a.window ||
                                           group_key[n] + 32 <= sink_keys))
           return;
+        if (__ballot(y.nan)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] = y.nan ? __builtin_nanf("") : x[i];
+        }
         // against the lane's first key, so that the others are constants
         const int first = group_key[n] + 4 * h, top = y.last - first;
         if (a.window == 0) {
@@ -671,10 +680,19 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void weight_tiles_kernel(WeightArgs
           const int row = span_rows.first + st * SR + t * 32 + col;
           const float l = lse_in[buf * 64 + t * 32 + col];
           y[t].last = s.first_own + wa.group.divide(min(row, span_rows.last - 1));
-          // a row that sees nothing, or is none, gives nothing
-          y[t].off = row < span_rows.last && l != NEG_INF ? l * LOG2E : -NEG_INF;
+          y[t].off = l * LOG2E;
+          y[t].nan = false;
           y[t].k0 = __builtin_amdgcn_readlane(y[t].last, 0);
           y[t].k1 = __builtin_amdgcn_readlane(y[t].last, 31);
+          // A row that sees nothing, or is none, gives nothing whatever its scores are: all its
+          // keys are hidden.  One whose lse is NaN gives that to the keys that it sees only.
+          const bool none = row >= span_rows.last || l == NEG_INF;
+          if (__ballot(none || l != l)) {
+            y[t].last = none ? -1 : y[t].last;
+            y[t].off = none || l != l ? 0.0f : y[t].off;
+            y[t].nan = l != l;
+            y[t].k0 = -1;
+          }
         }
         // A step is a row tile and 32 keys.  Its exponentials are taken beside the products of
         // the next: two sets of scores in turn.

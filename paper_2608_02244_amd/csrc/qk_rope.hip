@@ -254,44 +254,47 @@ __global__ __launch_bounds__(THREADS) void kv4_read_kernel(Read4Args a) {
   using G = Group4<D>;
   using elem = typename T::elem;
   constexpr int LANES = D / 8;
-  const int64_t at = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-  const int sub = (int)(at % LANES);
-  const int64_t v = at / LANES;  // token, side, head
-  const int kh = (int)(v % a.kv.kv_heads), side = (int)(v / a.kv.kv_heads & 1);
-  const int64_t t = v / a.kv.kv_heads >> 1;
-  if (t >= a.n_tok) return;
-  const int slot = a.slots[t], page = slot >> a.kv.page_shift;
-  const int off = slot & ((1 << a.kv.page_shift) - 1), tok = off & (GROUP - 1);
-  u32x4 x = {0, 0, 0, 0};
-  if (slot >= 0 && page < a.kv.n_pages) {
-    const char* group = (const char*)a.kv.k + page * a.kv.k_page + kh * a.kv.k_head +
-                        (off >> GROUP_SHIFT) * a.kv.k_slot;
-    uint32_t code;
-    if (side == 0) {
-      code = *(const uint32_t*)(group + G::key(tok) + sub * 4);
-    } else if constexpr (D == 64) {
-      code = *(const uint16_t*)(group + G::value(tok, 2 * sub)) |
-             (uint32_t)*(const uint16_t*)(group + G::value(tok, 2 * sub + 1)) << 16;
-    } else {
-      constexpr int PER = D / 128;
-      code = *(const uint32_t*)(group + G::value(tok, sub / PER) + sub % PER * 4);
+  const int64_t lanes = (int64_t)a.n_tok * a.kv.kv_heads * 2 * LANES;
+  for (int64_t at = (int64_t)blockIdx.x * THREADS + threadIdx.x; at < lanes;
+       at += (int64_t)gridDim.x * THREADS) {
+    const int sub = (int)(at % LANES);
+    const int64_t v = at / LANES;  // token, side, head
+    const int kh = (int)(v % a.kv.kv_heads), side = (int)(v / a.kv.kv_heads & 1);
+    const int64_t t = v / a.kv.kv_heads >> 1;
+    const int slot = a.slots[t], page = slot >> a.kv.page_shift;
+    const int off = slot & ((1 << a.kv.page_shift) - 1), tok = off & (GROUP - 1);
+    u32x4 x = {0, 0, 0, 0};
+    if (slot >= 0 && page < a.kv.n_pages) {
+      const char* group = (const char*)a.kv.k + page * a.kv.k_page + kh * a.kv.k_head +
+                          (off >> GROUP_SHIFT) * a.kv.k_slot;
+      uint32_t code;
+      if (side == 0) {
+        code = *(const uint32_t*)(group + G::key(tok) + sub * 4);
+      } else if constexpr (D == 64) {
+        code = *(const uint16_t*)(group + G::value(tok, 2 * sub)) |
+               (uint32_t)*(const uint16_t*)(group + G::value(tok, 2 * sub + 1)) << 16;
+      } else {
+        constexpr int PER = D / 128;
+        code = *(const uint32_t*)(group + G::value(tok, sub / PER) + sub % PER * 4);
+      }
+      const int byte = *(const uint8_t*)(group + (side == 0 ? G::key_scale(tok, sub >> 2)
+                                                            : G::value_scale(tok, sub >> 2)));
+      x = values8<T>(code, scale_of(byte));
+      if (byte == 255) {  // NaN
+        const uint32_t nan = pack2<T>(__builtin_nanf(""), __builtin_nanf(""));
+        x = (u32x4){nan, nan, nan, nan};
+      }
     }
-    const int byte = *(const uint8_t*)(group + (side == 0 ? G::key_scale(tok, sub >> 2)
-                                                          : G::value_scale(tok, sub >> 2)));
-    x = values8<T>(code, scale_of(byte));
-    if (byte == 255) {  // NaN
-      const uint32_t nan = pack2<T>(__builtin_nanf(""), __builtin_nanf(""));
-      x = (u32x4){nan, nan, nan, nan};
-    }
+    elem* out = (elem*)(side == 0 ? a.k_out : a.v_out);
+    *(u32x4*)(out + t * a.token + kh * a.head + sub * 8) = x;
   }
-  elem* out = (elem*)(side == 0 ? a.k_out : a.v_out);
-  *(u32x4*)(out + t * a.token + kh * a.head + sub * 8) = x;
 }
 
 template <class T, int D>
 void read(const Read4Args& a, hipStream_t s) {
   const int64_t lanes = (int64_t)a.n_tok * a.kv.kv_heads * 2 * (D / 8);
-  kv4_read_kernel<T, D><<<dim3((unsigned)((lanes + THREADS - 1) / THREADS)), THREADS, 0, s>>>(a);
+  const int64_t blocks = (lanes + THREADS - 1) / THREADS, most = 1 << 22;  // 2^30 threads
+  kv4_read_kernel<T, D><<<dim3((unsigned)(blocks < most ? blocks : most)), THREADS, 0, s>>>(a);
 }
 
 template <class T, int D, bool FP4>

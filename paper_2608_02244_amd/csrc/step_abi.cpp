@@ -312,7 +312,8 @@ int check_evict(const fsched_evict_params* p) {
     return FSCHED_EINVAL;
   if (p->page_size > kMaxPage || p->n_req > FSCHED_MAX_REQ) return FSCHED_ETOOLARGE;
   const int64_t row = (int64_t)p->table_width * p->page_size;
-  if (row > (1 << 30)) return FSCHED_ETOOLARGE;
+  // pages of all requests are counted in 32 bits
+  if (row > (1 << 30) || (int64_t)p->n_req * p->table_width > INT32_MAX) return FSCHED_ETOOLARGE;
   if (p->weight_stride < row) return FSCHED_EINVAL;
   return p->weight_stride > kMaxStride ? FSCHED_ETOOLARGE : FSCHED_OK;
 }

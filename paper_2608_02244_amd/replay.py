@@ -149,22 +149,21 @@ class Worker:
             (fs.attend4_weight if four else fs.attend_weight)(
                 q, lse, cache[0], self.table, q_start, kv_len, weight, **kw)
             out.append(y)
-        # only now: a step that ends with an error (in ``qkv``, say) can be run again
-        self.free = self.free[need:]
         held = [o + n for o, n in zip(old, new)]
+        table, freed, up = self.table, self.free[:0], [0] * len(held)
         if weight is not None:
-            self.attention = weight
             up = [self._given_up(m) for m in held]
             if any(up):
-                self.table, self.attention, _, freed, _ = fs.kv_evict(
-                    weight, kv_len, self.table, torch.full_like(kv_len, self.budget),
+                table, weight, _, freed, _ = fs.kv_evict(
+                    weight, kv_len, table, torch.full_like(kv_len, self.budget),
                     page_size=self.page_size, n_sink=self.n_sink, n_recent=self.n_recent,
                     n_freed=sum(up))
-                self.free = torch.cat((self.free, freed))
-                held = [m - u * self.page_size for m, u in zip(held, up)]
-                for r, u in zip(self.requests, up):
-                    self.gone[r] += u * self.page_size
-        self.held.update(zip(self.requests, held))
+        # only now: a step that ends with an error (in ``qkv``, say) can be run again
+        self.free = torch.cat((self.free[need:], freed))
+        self.table, self.attention = table, weight
+        for r, m, u in zip(self.requests, held, up):
+            self.held[r] = m - u * self.page_size
+            self.gone[r] += u * self.page_size
         return out
 
 

@@ -186,7 +186,8 @@ def test_store_refuses(kw, code):
     (dict(n_freed=-1), fs.EINVAL), (dict(reserved=1), fs.EINVAL),
     (dict(weight_stride=127), fs.EINVAL), (dict(n_req=4097), fs.ETOOLARGE),
     (dict(page_size=1 << 17, weight_stride=1 << 21), fs.ETOOLARGE),
-    (dict(table_width=1 << 27, weight_stride=1 << 31), fs.ETOOLARGE)])
+    (dict(table_width=1 << 27, weight_stride=1 << 31), fs.ETOOLARGE),
+    (dict(n_req=4096, table_width=1 << 19, weight_stride=1 << 23), fs.ETOOLARGE)])
 def test_evict_refuses(kw, code):
     assert evict(**kw) == code
     v = dict(n_req=4, table_width=8, page_size=16, n_freed=32, flags=DEV, weight_stride=128)

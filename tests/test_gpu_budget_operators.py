@@ -387,15 +387,76 @@ def test_attend4_rows_of_no_request_and_past_max_q_stay(dev):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("new", [[1, 1], [3, 60]], ids=["few", "many"])
+def test_attend4_not_finite_where_seen(dev, new):
+    """A block that stands for NaN makes NaN what it enters: a key's the rows that see it, a
+    value's its own elements of their outputs (and, as 0 * NaN, maybe those of other rows of
+    the request)."""
+    import torch
+    b = Batch4(dev, new, [50, 90], 8, 2, 128)
+    ref, ref_lse = (x.double().cpu() for x in b.call())
+    page, at = b.table[1, 3], 13  # token 61 of request 1
+    for side in ("key", "value"):
+        cache = b.cache.clone()
+        scales = (16 * 128 + at * 4 if side == "key" else 16 * 128 + 64 + at // 4 * 16 + at % 4)
+        cache[page, 1, 0, scales + (2 if side == "key" else 8)] = 255  # elements 64 .. 95
+        kw = {**b.kw}
+        out, lse = (x.double().cpu() for x in fs.attend4(b.args[0], cache, *b.args[3:], **kw))
+        bad = torch.zeros_like(ref, dtype=torch.bool)
+        sees = [new[0] + i for i in range(new[1]) if 90 - new[1] + i >= 48 + at]
+        bad[sees, 4:, (slice(None) if side == "key" else slice(64, 96))] = True
+        may = bad.clone()
+        if side == "value":
+            may[new[0]:, 4:, 64:96] = True
+        assert (out.isnan() | ~bad).all() and not (out.isnan() & ~may).any()
+        assert torch.equal(out[~may], ref[~may])
+        lost = bad.all(-1)
+        assert torch.equal(lse.isnan(), lost) and torch.equal(lse[~lost], ref_lse[~lost])
+
+
+def test_heads_requests_and_pages_at_their_most(dev):
+    """1,024 query heads on one and on as many; 4,096 requests; pages behind 2^32 bytes."""
+    import torch
+    Batch4(dev, [1, 2], [20, 37], 1024, 1, 64).check()
+    Batch4(dev, [1, 2], [20, 37], 1024, 1024, 64).check()
+    new = [1] * 4094 + [40, 20]
+    Batch4(dev, new, [m + i % 5 for i, m in enumerate(new)], 2, 1, 64).check()
+    H, page, D, n = 8, 64, 128, 300
+    few = fs.kv4_cache(6, H, page, D, device=dev).zero_()
+    many = fs.kv4_cache(80000, H, page, D, device=dev)  # 5.6 GB
+    g = torch.Generator(device=dev).manual_seed(1)
+    qkv = torch.randn(n, 32 + 2 * H, D, device=dev, generator=g).bfloat16()
+    pos = torch.arange(n, dtype=torch.int32, device=dev)
+    cs = torch.rand(n, D, device=dev, generator=g)
+    got = []
+    for cache, first in ((few, 0), (many, 80000 - 6)):
+        table = torch.arange(first, first + 6, dtype=torch.int32, device=dev).view(1, 6)
+        slots = pos + first * page
+        q = fs.qk_norm_rope4(qkv, pos, slots, cs, cache)
+        out = [q, *fs.kv4_read(cache, slots)]
+        for m in (1, n):
+            step = (torch.tensor([0, m], dtype=torch.int32, device=dev),
+                    torch.tensor([n], dtype=torch.int32, device=dev))
+            out += fs.attend4(q[:m], cache, table, *step, return_lse=True)
+            weight = torch.zeros(1, 6 * page, device=dev)
+            out.append(fs.attend4_weight(q[:m], out[-1], cache, table, *step, weight))
+        got.append(out)
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+
+
 # ------------------------------------------------------------------ the weight
 
-def check_weight(b, rows_apart=0, seed=0):
-    """Weights of a batch (of either kind) against 64 bits, and nothing else written."""
+def check_weight(b, rows_apart=0, seed=0, change=None):
+    """Weights of a batch (of either kind) against 64 bits, and nothing else written.
+    `change`: what a caller does with q and lse before the call."""
     import torch
     dev, page, n, Hq, grp = b.dev, b.page, len(b.own), b.Hq, b.Hq // b.Hkv
     log(f"attend_weight {type(b).__name__} new={b.new[:6]} own={b.own[:6]} n={n} heads={Hq}/"
         f"{b.Hkv} D={b.D} {b.dt} page={page} window={b.window}/{b.sinks} prefix={b.prefix}")
     lse = b.reference()[1].float()
+    if change:
+        change(b.q, lse)
+        b.args[0] = b.q.to(dev)
     row = b.table.shape[1] * page
     g = torch.Generator().manual_seed(seed)
     start = torch.rand(n, row + rows_apart, generator=g)
@@ -426,6 +487,11 @@ def check_weight(b, rows_apart=0, seed=0):
                 x, kk = b.q[a + i, h].double(), K[:, h // grp]
                 s = kk @ x * b.scale
                 at = lse[a + i, h].double()
+                if at == -math.inf:
+                    continue
+                if at.isnan():
+                    ref[r, :own] = torch.where(see, at, ref[r, :own])
+                    continue
                 w = torch.where(see, torch.exp(s - at), 0.0)
                 ref[r, :own] += w
                 size = (kk.abs() @ x.abs()) * b.scale
@@ -436,6 +502,8 @@ def check_weight(b, rows_apart=0, seed=0):
     untouched = ref == start.double()
     got = got.double().cpu()
     assert torch.equal(got[untouched], start.double()[untouched])
+    assert torch.equal(got.isnan(), ref.isnan())
+    got, ref, tol = (x.nan_to_num(0.0) for x in (got, ref, tol))
     assert ((got - ref).abs() <= tol).all(), ((got - ref).abs() - tol).max()
 
 
@@ -508,6 +576,30 @@ def test_weight_many_requests_long_rows_and_equal_bits(dev, kind):
         assert torch.equal(w, got[0])
     # every row's weights sum to one
     assert abs(float(got[0].sum()) / (341 * 4) - 1) < 2.0 ** -16
+
+
+@pytest.mark.parametrize("kind", [Batch, Batch4], ids=["16bit", "4bit"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
+def test_weight_rows_left_out_and_not_finite(dev, kind, window, sinks):
+    """A row whose lse is -infinity gives nothing, whatever it holds; one whose lse is NaN
+    gives NaN to the keys that it sees, and to no others."""
+    def change(q, lse):
+        q[0, 1], lse[0, 1] = math.nan, -math.inf
+        q[2], lse[2] = math.inf, -math.inf          # a token of the few
+        lse[3, 5] = math.nan
+        q[14, 3], lse[14, 3] = math.nan, -math.inf  # and of the many
+        lse[20], lse[70, 0] = -math.inf, math.nan
+        q[83], lse[83] = math.nan, -math.inf        # the last of a tile's rows
+    check_weight(kind(dev, [1, 3, 80], [40, 50, 200], 8, 2, 64, window=window, sinks=sinks),
+                 change=change)
+
+
+@pytest.mark.parametrize("kind", [Batch, Batch4], ids=["16bit", "4bit"])
+def test_weight_many_heads_and_most_requests(dev, kind):
+    check_weight(kind(dev, [1, 2], [20, 37], 1024, 1, 64))
+    check_weight(kind(dev, [1, 2], [20, 37], 1024, 1024, 64))
+    new = [1] * 4094 + [40, 20]
+    check_weight(kind(dev, new, [m + i % 5 for i, m in enumerate(new)], 2, 1, 64))
 
 
 # ---------------------------------------------------------------- the eviction
@@ -667,6 +759,31 @@ def test_step_within_a_budget_in_a_captured_graph(dev):
         b = one()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_two_streams_at_once(dev):
+    """Calls of two streams overlap and give what each gives alone."""
+    import torch
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    batches = [Batch4(dev, [1] * 20 + [70], [300 + 7 * i for i in range(20)] + [400], 8, 2, 128,
+                      seed=i) for i in range(2)]
+
+    def calls(b, stream=None):
+        out, lse = b.call(stream=stream)
+        w = torch.zeros(21, b.table.shape[1] * 16, device=dev)
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        kw = dict(scale=b.scale, max_q=70, stream=stream)
+        fs.attend4_weight(b.args[0], lse, b.cache, *b.args[3:], w, **kw)
+        return (out, lse, w, *fs.kv_evict(w, b.args[5], b.args[3], b.args[5] // 2, page_size=16,
+                                          n_sink=2, n_recent=40, stream=stream))
+    alone = [calls(b) for b in batches]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        both = [calls(b, s) for b, s in zip(batches, streams)]
+        torch.cuda.synchronize()
+        for x, y in zip(alone, both):
+            assert all(torch.equal(p, q) for p, q in zip(x, y))
 
 
 @pytest.mark.parametrize("bits", [16, 4])
