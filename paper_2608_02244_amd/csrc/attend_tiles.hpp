@@ -239,33 +239,37 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
     auto place = [&](int key, int piece) {
       return to + key * (D * 2) + (piece ^ L::swizzle(key)) * 16;
     };
+    // The places of neighbouring keys and pieces differ in few bits of the swizzle: they are
+    // made from one place each time, since a register for each costs a block per unit.
     const float ks = scale_of(t.k_scale);
+    const uint32_t k_to = place(my_key, tid % Raw::SHARE * Raw::WORDS);
 #pragma unroll
-    for (int i = 0; i < Raw::WORDS; ++i)
-      write16(place(my_key, tid % Raw::SHARE * Raw::WORDS + i), values8<T>(t.k[i], ks));
-    const int key = my_quarter * 4;
+    for (int i = 0; i < Raw::WORDS; ++i) write16(k_to ^ (i * 16), values8<T>(t.k[i], ks));
     auto scale = [&](int j) { return scale_of((t.v_scale >> (8 * j)) & 255); };
     if constexpr (D == 64) {  // two bytes of each token: half a 16-byte piece
-      const uint32_t at = L::BYTES + (my_piece & 1) * 8;
+      const uint32_t v_to = place(my_quarter * 4, my_piece >> 1) + (my_piece & 1) * 8;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t c = t.v[j >> 1];
         const float s = scale(j);
         const u32x2 y = j & 1 ? (u32x2){values2<T, 2>(c, s), values2<T, 3>(c, s)}
                               : (u32x2){values2<T, 0>(c, s), values2<T, 1>(c, s)};
-        write8(place(key + j, my_piece >> 1) + at, y);
+        write8((v_to ^ (L::swizzle(j) * 16)) + L::BYTES + j * (D * 2), y);
       }
     } else if constexpr (D == 128) {
+      const uint32_t v_to = place(my_quarter * 4, my_piece);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        write16(place(key + j, my_piece) + L::BYTES, values8<T>(t.v[j], scale(j)));
+        write16((v_to ^ (L::swizzle(j) * 16)) + L::BYTES + j * (D * 2),
+                values8<T>(t.v[j], scale(j)));
     } else {  // 8 bytes of two tokens
+      const uint32_t v_to = place(my_quarter * 4 + 2 * my_half, 2 * my_piece);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const float s = scale_of((t.v_scale >> (16 * my_half + 8 * j)) & 255);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          write16(place(key + 2 * my_half + j, 2 * my_piece + i) + L::BYTES,
+          write16((v_to ^ (L::swizzle(j) * 16) ^ (i * 16)) + L::BYTES + j * (D * 2),
                   values8<T>(t.v[2 * j + i], s));
       }
     }
