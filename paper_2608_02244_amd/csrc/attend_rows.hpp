@@ -45,6 +45,7 @@ struct RowsPlan {
   int32_t slot_rows;    // rows of a part's slot
   int32_t most_parts;   // of a tile, on average
   int32_t keep_parts;   // 1: results join with those of the prefix, written as parts
+  int32_t whole;        // 1: no tile is cut (a cache of 4 bits; nothing to join then)
   float* part_o;        // [slots][slot_rows][head_dim]; slots: 2 per wave, then with
                         // keep_parts one per tile, for those that lie in one piece
   float2* part_ml;      // [slots][slot_rows] (mu, l)
@@ -179,6 +180,14 @@ __device__ __forceinline__ RowsPart rows_part(const AttnArgs& a, const RowsLine&
   p.u0 = (int)(rest - l.before[lo]);
   p.u1 = (int)min((int64_t)p.units, p.u0 + (l.end - w));
   return p;
+}
+
+// The first unit from w on that begins a tile.
+__device__ __forceinline__ int64_t rows_tile_from(const AttnArgs& a, const RowsLine& l,
+                                                  int64_t w) {
+  if (w >= l.total) return l.total;
+  const RowsPart p = rows_part(a, l, w);
+  return p.u0 == 0 ? w : w - p.u0 + p.units;
 }
 
 // A part's end: the result of a tile that lies whole in the wave's piece, else a part for

@@ -45,8 +45,12 @@ __device__ __forceinline__ void attend_rows4(const AttnArgs& a, const RowsPlan& 
   const uint32_t ks_lane = G::key_scale(col, h * (D / 4) / 32);
   const uint32_t vs_lane = G::value_scale(4 * h, col * DL / 32);
 
-  const RowsLine line = rows_line(a, plan, 16 * RT, block, lds);
+  RowsLine line = rows_line(a, plan, 16 * RT, block, lds);
   if (line.me >= line.waves) return;
+  if (plan.whole) {  // the tiles that begin in this wave's piece
+    line.begin = rows_tile_from(a, line, line.begin);
+    line.end = rows_tile_from(a, line, line.end);
+  }
   for (int64_t w = line.begin; w < line.end;) {
     const RowsPart part = rows_part(a, line, w);
     const int kh = part.kh, u0 = part.u0, u1 = part.u1;

@@ -297,6 +297,26 @@ def test_attend4_window(dev, window, sinks):
 
 
 @pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("page", [16, 64])
+def test_attend4_short_tables(dev, D, page):
+    """Tables of at most 128 keys, and of the next size: few requests and many, drafts."""
+    import torch
+    own = [1, 0, 16, 17, 33, 64, 48, 2, 31, 50, 60, 5]
+    for most in (1, 33, 64, 112, 113, 128):
+        Batch4(dev, [1] * 11 + [0], [min(m, most) for m in own] if most <= 64 else own[:-1] + [most],
+               8, 2, D, page=page, seed=most).check()
+    Batch4(dev, [1, 3, 2], [40, 3, 60], 10, 2, D, page=page).check()
+    Batch4(dev, [1] * 12, own, 8, 2, D, page=page, window=20, sinks=3).check()
+    b = Batch4(dev, [1] * 900, [i % 60 for i in range(900)], 16, 8, D, page=page)
+    b.table[5::7, 0] = -1
+    b.args[3] = b.table.to(dev)
+    b.check()
+    w = fs.attend4_workspace(900, 900, 16, 8, D, page_size=page, table_width=b.table.shape[1],
+                             max_q=1)
+    assert all(torch.equal(x, y) for x, y in zip(b.call(workspace=w), b.call()))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("heads", [(4, 4), (8, 1), (10, 2)], ids=lambda h: f"{h[0]}x{h[1]}")
 def test_attend4_few_and_many_new_tokens(dev, D, heads):
     """Drafts, whole prompts, chunks behind a held part, decoding requests among them."""
