@@ -16,7 +16,10 @@
 //
 // Into a cache of 4 bits, keys are normed and rotated in 64 bits, so that their codes are
 // those of the numbers themselves and not of one order of summing them: a number next to
-// the border of two codes is off by a third of itself on the other side.
+// the border of two codes is off by a third of itself on the other side.  Bound by these
+// instructions beside the bytes: 32,771 tokens of 48 heads of 128 (f16), 174 us for the
+// store (72 % of the vector issue; 186 with the norm of keys and values taken in 32 bits too)
+// and 42 for reading them back, 5.2 TB/s; 64 tokens, 4.8 and 2.8 us.
 #include <hip/hip_runtime.h>
 
 #include "fp4.hpp"
@@ -83,6 +86,8 @@ __device__ __forceinline__ void exact_key(typename T::x8 raw, const void* weight
 }
 
 // FP4: the cache holds 4 bits an element; its strides are bytes, k_slot that of a group.
+// Six blocks per compute unit then (80 registers): stored and read back, the case above
+// 202 us with 6, 214 with 5, 207 with 8.
 template <class T, int D, bool INTER, bool FP4>
 __global__ __launch_bounds__(THREADS, FP4 ? 6 : 1) void qk_rope_kernel(RopeArgs a, int chunks,
                                                                       int per_chunk) {
