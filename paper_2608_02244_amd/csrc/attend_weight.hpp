@@ -136,7 +136,8 @@ weight_rows_kernel(WeightArgs wa) {
   // Where there are fewer units than half or a quarter of the waves, two or four waves of a
   // block share a unit's key heads.
   const int64_t waves = (int64_t)gridDim.x * ATT_WAVES;
-  const int shares = 4 * total <= waves ? 4 : 2 * total <= waves ? 2 : 1;
+  const int heads = a.kv.kv_heads;  // (each share has one at least)
+  const int shares = 4 * total <= waves && heads >= 4 ? 4 : 2 * total <= waves && heads >= 2 ? 2 : 1;
   const int64_t me = (int64_t)blockIdx.x * ATT_WAVES + wave, mine = me / shares;
   const int share = (int)(me % shares);
   int64_t begin = mine, end = min(mine + 1, total);
@@ -236,88 +237,101 @@ weight_rows_kernel(WeightArgs wa) {
       }
       return k;
     };
-    struct Rows {
+    struct Item {  // a unit and a key head, heads first
+      Keys k;
       x8 q[RT][KC];
       float lse[RT];
     };
-    auto rows_at = [&](int kh) {
-      Rows y;
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        const elem* src = q_at[t] + (int64_t)kh * a.group * a.q_head;
-#pragma unroll
-        for (int c = 0; c < KC; ++c)
-          y.q[t][c] = *(const x8*)(src + (FP4 ? c * 8 : (c >> 1) * 64 + (c & 1) * 8));
-        y.lse[t] = lse_at[t][kh * a.group];
-      }
-      return y;
-    };
-
-    // items: a unit and a key head, heads first; the next item is under way
-    int pages[2], later[2];
+    // Two items are under way while one is worked on: its place is loaded again as soon as
+    // the products have read it.
+    int pages[2], later[2], fetch_u = u0, fetch_kh = kh0;
     const char* at[2];
     pages_of(u0, pages);
     places(u0, pages, at);
-    Keys next = load(at, kh0);
-    Rows next_rows = rows_at(kh0);
     if (u0 + 1 < u1) pages_of(u0 + 1, later);
-    for (int u = u0; u < u1; ++u) {
+    auto fetch = [&](Item& y) {
+      if (fetch_u >= u1) return;
+      y.k = load(at, fetch_kh);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const elem* src = q_at[t] + (int64_t)fetch_kh * a.group * a.q_head;
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+          y.q[t][c] = *(const x8*)(src + (FP4 ? c * 8 : (c >> 1) * 64 + (c & 1) * 8));
+        y.lse[t] = lse_at[t][fetch_kh * a.group];
+      }
+      if (++fetch_kh == kh1) {
+        fetch_kh = kh0;
+        if (++fetch_u < u1) {
+          places(fetch_u, later, at);
+          if (fetch_u + 1 < u1) pages_of(fetch_u + 1, later);
+        }
+      }
+    };
+    int u = u0, kh = kh0, here[2];
+    float sum[2][4] = {};
+    // lane `col` < 8 of each row of lanes has key 16 (col / 4) + 4h + col mod 4 of a unit
+    const int j = (col >> 2) * 16 + 4 * h + (col & 3);
+    float old = 0.0f;
+    auto begin_unit = [&]() {  // its pages and old weights, for the write behind its last head
+      pages_of(u, here);
+      const int key = sp.block(u) * WEIGHT_UNIT + j;
+      old = 0.0f;
+      if (col < 8 && seen(key)) old = wa.weight[(int64_t)r * wa.weight_stride + key];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[b][e] = 0.0f;
+    };
+    auto work = [&](Item& now) {
       const int s0 = sp.block(u) * WEIGHT_UNIT;
       const bool full = s0 + WEIGHT_UNIT - 1 <= first_own &&
                         (a.window == 0 || s0 > last_own - a.window ||
                          s0 + WEIGHT_UNIT <= sink_keys);
-      const int here[2] = {pages[0], pages[1]};
-      float sum[2][4] = {};
-      for (int kh = kh0; kh < kh1; ++kh) {
-        const Keys now = next;
-        const Rows mine_now = next_rows;
-        if (kh + 1 < kh1) {
-          next = load(at, kh + 1);
-          next_rows = rows_at(kh + 1);
-        } else if (u + 1 < u1) {
-          pages[0] = later[0];
-          pages[1] = later[1];
-          places(u + 1, pages, at);
-          next = load(at, kh0);
-          next_rows = rows_at(kh0);
-          if (u + 2 < u1) pages_of(u + 2, later);
+      x8 k[2][KC];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          if constexpr (FP4) {
+            const uint32_t byte = D == 256 ? (now.k.scale[b] >> (c / 4 * 8)) & 255 : now.k.scale[b];
+            k[b][c] = __builtin_bit_cast(x8, values8<T>(now.k.w[b][c], scale_of(byte)));
+          } else {
+            k[b][c] = __builtin_bit_cast(x8, (u32x4){now.k.w[b][4 * c], now.k.w[b][4 * c + 1],
+                                                     now.k.w[b][4 * c + 2], now.k.w[b][4 * c + 3]});
+          }
         }
-        x8 k[2][KC];
+      f32x4 s[RT][2];
+      float lse[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        lse[t] = now.lse[t];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          s[t][b] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+          for (int c = 0; c < KC; ++c) s[t][b] = T::mfma16(k[b][c], now.q[t][c], s[t][b]);
+        }
+      }
+      fetch(now);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        // a row that sees nothing, or is none, gives nothing
+        const bool some = on[t] && lse[t] != NEG_INF;
+        const float off = lse[t] * LOG2E;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int c = 0; c < KC; ++c) {
-            if constexpr (FP4) {
-              const uint32_t byte = D == 256 ? (now.scale[b] >> (c / 4 * 8)) & 255 : now.scale[b];
-              k[b][c] = __builtin_bit_cast(x8, values8<T>(now.w[b][c], scale_of(byte)));
-            } else {
-              k[b][c] = __builtin_bit_cast(x8, (u32x4){now.w[b][4 * c], now.w[b][4 * c + 1],
-                                                       now.w[b][4 * c + 2], now.w[b][4 * c + 3]});
-            }
+          for (int e = 0; e < 4; ++e) {
+            const float p = exp2_fast(fmaf(s[t][b][e], a.scale_log2, -off));
+            const int key = s0 + b * 16 + 4 * h + e;
+            const bool see =
+                some && (full || (key <= top[t] && (key > low[t] || key < sink_keys)));
+            sum[b][e] += see ? p : 0.0f;
           }
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          // a row that sees nothing, or is none, gives nothing
-          const float l = mine_now.lse[t];
-          const bool some = on[t] && l != NEG_INF;
-          const float off = l * LOG2E;
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            f32x4 s = {0, 0, 0, 0};
-#pragma unroll
-            for (int c = 0; c < KC; ++c) s = T::mfma16(k[b][c], mine_now.q[t][c], s);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float p = exp2_fast(fmaf(s[e], a.scale_log2, -off));
-              const int key = s0 + b * 16 + 4 * h + e;
-              const bool see =
-                  some && (full || (key <= top[t] && (key > low[t] || key < sink_keys)));
-              sum[b][e] += see ? p : 0.0f;
-            }
-          }
-        }
       }
-      // lane `col` < 8 of each row of lanes has key 16 (col / 4) + 4h + col mod 4
+      if (++kh < kh1) return;
+      kh = kh0;
       float v = 0.0f;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -326,7 +340,7 @@ weight_rows_kernel(WeightArgs wa) {
           const float y = sum_row16(sum[b][e]);
           v = col == b * 4 + e ? y : v;
         }
-      const int j = (col >> 2) * 16 + 4 * h + (col & 3), key = s0 + j;
+      const int key = s0 + j;
       int page = col < 4 ? here[0] : here[1];
       if constexpr (!WIDE) {  // the lane that looked this key up
         const int p0 = __shfl(here[0], j & 15), p1 = __shfl(here[1], j & 15);
@@ -335,8 +349,17 @@ weight_rows_kernel(WeightArgs wa) {
       const bool writes = col < 8 && seen(key) && (uint32_t)page < (uint32_t)a.kv.n_pages;
       out = writes ? wa.weight + (int64_t)r * wa.weight_stride + key : nullptr;
       value = v;
-      if (shares == 1 && out) *out += v;
+      if (shares == 1 && out) *out = old + v;
       if (shares > 1 && col < 8) shared_sum[wave][j] = v;
+      if (++u < u1) begin_unit();
+    };
+    Item ring[2];
+    fetch(ring[0]);
+    fetch(ring[1]);
+    begin_unit();
+    while (u < u1) {
+      work(ring[0]);
+      if (u < u1) work(ring[1]);
     }
   }
   if (shares == 1) return;
