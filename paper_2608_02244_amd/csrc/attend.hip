@@ -135,10 +135,13 @@ __global__ __launch_bounds__(THREADS) void attend_join_kernel(AttnArgs a, JoinAr
   }
 }
 
-// Requests whose tables hold at most this many keys are not cut over a cache of 4 bits: there
-// is no join to launch then.  Cut / whole, us, requests of 1 to 64, 128 and 256 keys, 8 key
-// heads: 8 requests 10.4 / 8.4, 10.3 / 9.2, 10.9 / 13.7; 64 requests 11.3 / 9.0, 12.9 / 12.8,
-// 15.6 / 20.0; 512 requests 27.6 / 22.6, 33.9 / 27.4, 41.1 / 37.5.
+// Requests whose tables hold at most this many keys (twice as many where there are tiles for
+// half the waves) are not cut over a cache of 4 bits: there is no join to launch then.  Cut /
+// whole, us, requests of 1 to 64, 128, 256 and 512 keys, 8 key heads:
+//     8 requests  10.4 /  8.4   10.3 /  9.2   10.9 / 13.7   11.7 / 20.4
+//    64 requests  11.3 /  9.0   12.9 / 12.8   15.6 / 20.0   20.1 / 29.3
+//   256 requests  19.7 / 15.2   24.7 / 18.2   30.0 / 27.1   38.0 / 41.8
+//   512 requests  27.6 / 22.6   33.9 / 27.4   41.1 / 37.5   57.8 / 59.7
 constexpr int WHOLE_KEYS = 128;
 
 // What a call of this shape launches, and where its workspace's parts lie.
@@ -183,8 +186,9 @@ Shape plan(const AttnArgs& a, bool fp4, int head_dim, int n_cu, char* ws) {
     rp.waves = p.main.rows_blocks * ATT_WAVES;
     rp.most_parts = fp4 ? MOST_PARTS4 : MOST_PARTS;
     rp.keep_parts = prefix;
+    const int64_t keys = (int64_t)a.width << a.kv.page_shift;
     rp.whole = fp4 && !prefix && !with_tiles &&
-               ((int64_t)a.width << a.kv.page_shift) <= WHOLE_KEYS;
+               keys <= (2 * (int64_t)a.n_req * a.kv.kv_heads < rp.waves ? 1 : 2) * WHOLE_KEYS;
     rp.slot_rows = most < limit ? (int)most : limit;
     const size_t whole = prefix ? (size_t)a.n_req * a.kv.kv_heads : 0;
     const size_t slots = (2 * (size_t)rp.waves + whole) * rp.slot_rows;

@@ -16,8 +16,8 @@
 // rows, whose sums are then joined, in their order, by a second launch.  Equal calls give
 // equal bits.
 //
-// Measured (heads of 128, bf16): 64 requests holding 65,000 tokens, 32 us or 4.2 TB/s; 512
-// holding 0.73 M in 4 bits, 61 us or 3.4 TB/s; prompts of 25,600 tokens, 366 us or 820
+// Measured (heads of 128, bf16): 64 requests holding 65,000 tokens, 31 us or 4.3 TB/s; 512
+// holding 0.73 M in 4 bits, 59 us or 3.5 TB/s (4.1 without the start); prompts of 25,600 tokens, 366 us or 820
 // TFLOP/s (beside them 5 us of requests with few rows and 6 of joins).
 #pragma once
 #include <hip/hip_runtime.h>
