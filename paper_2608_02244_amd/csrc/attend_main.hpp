@@ -33,9 +33,10 @@ attend_rows_kernel(AttnArgs a, MainPlan p) {
 }
 
 // Blocks per compute unit that registers have to leave room for.  Heads of 64 over a cache of
-// 4 bits with 3 rather than 2, us: prompts of 25,600 tokens 409 : 464, chunks beside decoding
-// requests 64.5 : 67.3 and 78.5 : 78.1, one prompt 117 : 106 (all its blocks at once, none
-// left to even out the units).  Over a 16-bit cache they have 3 by themselves.
+// 4 bits with 3 rather than 2, us, at that stage of the kernels: prompts of 25,600 tokens 409 :
+// 464, chunks beside decoding requests 64.5 : 67.3 and 78.5 : 78.1, one prompt 117 : 106 (all
+// its blocks at once, none left to even out the units).  Over a 16-bit cache they have 3 by
+// themselves.
 constexpr int tiles_occupancy(int D, int KIND) {
   return D == 256 ? 1 : D == 64 && KIND == FP4_PAGES ? 3 : 2;
 }

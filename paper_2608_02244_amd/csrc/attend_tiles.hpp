@@ -545,16 +545,21 @@ __device__ __forceinline__ void attend_tiles(const AttnArgs& a, const TilesPlan&
     for (int d = 0; d < DT; ++d) vf[0][d] = values(0, d);
     __builtin_amdgcn_sched_barrier(0);
     if (!full) {
-      const uint64_t mine = found >> (4 * h);
+      // the tile's keys that the lane's row sees, as bits: tested one by one they take less
+      // than half the instructions of three comparisons each (chunks beside decoding requests
+      // with a window, heads of 64 in 4 bits: 65.4 -> 59.8 us)
+      auto below = [](int n) {  // bits 0 .. n - 1
+        return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
+      };
+      uint64_t mine = found & below(top - s0 + 1);
+      if (a.window > 0) mine &= ~below(low - s0 + 1) | below(sink_keys - s0);
+      mine >>= 4 * h;
+      const uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int at = t * 32 + 8 * (i / 4) + (i % 4), key = s0 + at + 4 * h;
-          const bool see = (bool)((mine >> at) & 1) & (key <= top) &
-                           ((key > low) | (key < sink_keys));
-          s[t][i] = see ? s[t][i] : NEG_INF;
-        }
+        for (int i = 0; i < 16; ++i)
+          s[t][i] = half[t] & (1u << (8 * (i / 4) + (i % 4))) ? s[t][i] : NEG_INF;
     }
     float mx = NEG_INF;
 #pragma unroll
