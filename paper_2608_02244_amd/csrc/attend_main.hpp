@@ -32,18 +32,9 @@ attend_rows_kernel(AttnArgs a, MainPlan p) {
   rows_block<T, D, RT, KIND>(a, p.rows, blockIdx.x, lds);
 }
 
-// Blocks per compute unit that registers have to leave room for.  Heads of 64 over a cache of
-// 4 bits with 3 rather than 2, us, at that stage of the kernels: prompts of 25,600 tokens 409 :
-// 464, chunks beside decoding requests 64.5 : 67.3 and 78.5 : 78.1, one prompt 117 : 106 (all
-// its blocks at once, none left to even out the units).  Over a 16-bit cache they have 3 by
-// themselves.
-constexpr int tiles_occupancy(int D, int KIND) {
-  return D == 256 ? 1 : D == 64 && KIND == FP4_PAGES ? 3 : 2;
-}
-
 template <class T, int D, int KIND>
-__global__ __launch_bounds__(ATT_THREADS, tiles_occupancy(D, KIND)) void attend_tiles_kernel(
-    AttnArgs a, MainPlan p) {
+__global__ __launch_bounds__(ATT_THREADS, D == 256 ? 1 : 2) void attend_tiles_kernel(AttnArgs a,
+                                                                                     MainPlan p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int b = blockIdx.x;
   const bool pre = b < p.pre_blocks;
@@ -51,8 +42,8 @@ __global__ __launch_bounds__(ATT_THREADS, tiles_occupancy(D, KIND)) void attend_
 }
 
 template <class T, int D, int RT, int KIND>
-__global__ __launch_bounds__(ATT_THREADS, tiles_occupancy(D, KIND)) void attend_both_kernel(
-    AttnArgs a, MainPlan p) {
+__global__ __launch_bounds__(ATT_THREADS, D == 256 ? 1 : 2) void attend_both_kernel(AttnArgs a,
+                                                                                    MainPlan p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int b = blockIdx.x;
   if (b < p.rows_blocks) {
