@@ -78,6 +78,9 @@ __device__ __forceinline__ Span span_of(int p0, int p1, int n, int window, int n
 }
 
 __device__ __forceinline__ int uni_int(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ Request uniform_request(const Request& x) {
+  return Request{uni_int(x.q0), uni_int(x.q_len), uni_int(x.kv)};
+}
 
 // Largest and summed value over the lanes that hold parts of one row: lanes
 // equal mod 32 (xor 32), or mod 16 (xor 16 and 32).

@@ -54,9 +54,10 @@ __device__ __forceinline__ void attend_rows4(const AttnArgs& a, const RowsPlan& 
   }
   for (int64_t w = line.begin; w < line.end;) {
     const RowsPart part = rows_part(a, line, w);
-    const int kh = part.kh, u0 = part.u0, u1 = part.u1;
+    // the same in all lanes, and places from them too: scalars
+    const int kh = uni_int(part.kh), u0 = uni_int(part.u0), u1 = uni_int(part.u1);
     const int r = uni_int(part.r);
-    const Request x = request_of(a, r);
+    const Request x = uniform_request(request_of(a, r));
     const Span sp = rows_span(a, x);
     const int rows = rows_of(a, x);
     const int first_own = x.kv - x.q_len;           // own index of the first token
