@@ -65,7 +65,7 @@ class Worker:
         self.table = torch.empty(0, self.width, dtype=torch.int32, device=device)
         # attention weight of held tokens, one row per row of the table
         self.attention = None if budget is None else \
-            torch.empty(0, self.width * page_size, device=device)
+            torch.empty(0, self.width * page_size, dtype=torch.float32, device=device)
 
     def _pages(self, tokens: int) -> int:
         return -(-tokens // self.page_size)

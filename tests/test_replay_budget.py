@@ -184,3 +184,19 @@ def test_a_schedule_plays_within_a_budget(plain):
                         lambda t, now, out: seen.append(list(now)), lengths=[30, 7])
     assert steps == 30 and sum(map(len, seen)) == 37
     assert not w.requests and sorted(w.free.tolist()) == list(range(40))
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float16, torch.float64])
+def test_attention_weights_are_float32_under_any_default_type(plain, default):
+    """attend_weight adds to 32-bit numbers only, whatever a program makes torch's default."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(default)
+    try:
+        w = worker(budget=4)
+        w.admit([0, 1])
+        w.step([9, 2], lambda layer: projection(11))
+        w.release([1])
+        w.admit([2])
+        assert w.attention.dtype == torch.float32 and w.cos_sin.dtype == torch.float32
+    finally:
+        torch.set_default_dtype(before)
