@@ -188,8 +188,8 @@ def _workspace(name, c, n_tok, n_req, q_heads, table_width, max_q, prefix_len, w
 def kv4_cache(n_pages: int, kv_heads: int, page_size: int, head_dim: int, *, device="cuda"):
     """An empty cache of 4 bits an element (its contents are undefined): uint8 [n_pages,
     kv_heads, page_size / 16, 17 head_dim], keys and values."""
-    if page_size < 16 or page_size % 16:
-        raise ValueError("a cache of 4 bits has pages of 16 tokens and more, a power of two")
+    if not 16 <= page_size <= 65536 or page_size & (page_size - 1):
+        raise ValueError("a cache of 4 bits has pages of 16 to 65,536 tokens, a power of two")
     return torch.empty(n_pages, kv_heads, page_size // 16, 17 * head_dim, dtype=torch.uint8,
                        device=device)
 

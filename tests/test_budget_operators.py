@@ -267,3 +267,11 @@ def test_binding_refuses_streams_and_what_is_no_tensor():
         for call in calls(first):
             with pytest.raises(ValueError, match="must be a"):
                 call()
+
+
+@pytest.mark.parametrize("page", [0, -16, 8, 48, 80, 96, 131072])
+def test_cache_of_pages_that_every_call_refuses_is_not_made(page):
+    with pytest.raises(ValueError, match="power of two"):
+        fs.kv4_cache(3, 2, page, 64, device="cpu")
+    for page in (16, 64, 65536):
+        assert fs.kv4_cache(1, 1, page, 64, device="cpu").shape == (1, 1, page // 16, 17 * 64)
