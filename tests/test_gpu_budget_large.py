@@ -1,7 +1,7 @@
 """The operators of a KV cache within a budget where the work fills the card several times
-over: attention weights whose blocks go through many units, key heads and tiles.  References
-are in 64 bits, request by request; what has to be large is computed from the shapes and
-asserted.
+over: attention weights whose blocks go through many units, key heads and tiles, and
+evictions from rows that one block does not hold.  References are in 64 bits, request by
+request; what has to be large is computed from the shapes and asserted.
 
 Tolerance of a weight, fixed before any run: as for small batches (w (e + 2^-22 (|s| + |lse|))
 + 2^-23 |weight|, e = (D + 8) 2^-24 scale sum_d |q_d k_d|), but the sum of a key's n terms is
@@ -16,6 +16,7 @@ import math
 import pytest
 
 import paper_2608_02244_amd as fs
+from test_gpu_budget_operators import check_evict
 from test_gpu_step_operators import dev, dtype_of, log  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -232,3 +233,29 @@ def test_weight_tiles_of_many_short_prompts(dev, bits, D, heads):
     """Pieces of several tiles: some whole in one, others at both of its ends."""
     new = [40 + 29 * i % 211 for i in range(800)]
     check_tiles(Large(dev, new, new, *heads, D, "bf16", bits, 16), whole=True)
+
+
+# --------------------------------------------- evictions in more than one launch
+
+# (page, width): rows that one block holds and the next size, by tokens (32,768) and by
+# pages (4,096)
+ROWS = [(8, 4096), (8, 4097), (1, 4097), (2, 4097), (4, 8193), (16, 2048), (16, 2049), (64, 513),
+        (128, 257), (256, 129)]
+
+
+@pytest.mark.parametrize("page,width", ROWS)
+@pytest.mark.parametrize("levels,holes,apart", [(0, 0.0, 0), (2, 0.2, 3), (0, 0.1, 3), (3, 0.0, 0)])
+def test_evict_rows_past_one_block(dev, page, width, levels, holes, apart):
+    """Requests of uneven length, an empty one and one within its budget among them."""
+    row = width * page
+    kv = [row, 0, row - 3, 2 * page + 1, 2 * row // 3]
+    budget = [row // 2, 5, row - 5 * page, row, 3]
+    check_evict(dev, kv, width, page, budget, sinks=3, recent=page + 9, seed=page, levels=levels,
+                holes=holes, rows_apart=apart)
+
+
+def test_evict_rows_past_one_block_with_nothing_to_drop(dev):
+    check_evict(dev, [33000, 40, 0], 2100, 16, 33000, sinks=3, recent=9, levels=2)
+    check_evict(dev, [33000, 33600], 2100, 16, 10, sinks=10 ** 9, levels=2)
+    check_evict(dev, [33000, 33600], 2100, 16, 10, recent=2 ** 31 - 1, n_freed=5, levels=2)
+    check_evict(dev, [33000, 33600, 20000], 2100, 16, 0, n_freed=100, rows_apart=1)
