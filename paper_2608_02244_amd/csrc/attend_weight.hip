@@ -36,8 +36,8 @@ Shape shape_of(const WeightArgs& a, int head_dim, int n_cu, char* ws) {
 template <class T, int D, int KIND>
 hipError_t launch_kind(const WeightArgs& a, const Shape& p, int n_cu, hipStream_t s) {
   const size_t line = (size_t)(ATT_WAVES + a.at.n_req + 1) * sizeof(int64_t);
+  constexpr bool FP4 = KIND == FP4_PAGES;
   if (p.few) {
-    constexpr bool FP4 = KIND == FP4_PAGES;
     if (most_rows(a) <= 16)
       weight_rows_kernel<T, D, 1, KIND>
           <<<(unsigned)(weight_occupancy(D, 1, FP4) * n_cu), ATT_THREADS, line, s>>>(a);
@@ -49,7 +49,7 @@ hipError_t launch_kind(const WeightArgs& a, const Shape& p, int n_cu, hipStream_
   }
   using L = WeightTileOf<D>;
   const size_t lds = L::LDS + line;
-  void (*kernel)(WeightArgs, WeightPlan) = weight_tiles_kernel<T, D, KIND>;
+  void (*kernel)(WeightArgs, WeightPlan) = weight_tiles_kernel<T, D, FP4>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(
         (const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -81,7 +81,7 @@ hipError_t launch_dim(const WeightArgs& a, bool fp4, int head_dim, const Shape& 
 
 }  // namespace
 
-size_t weight_workspace(const WeightArgs& a, bool, int head_dim, int n_cu) {
+size_t weight_workspace(const WeightArgs& a, int head_dim, int n_cu) {
   return shape_of(a, head_dim, n_cu > 0 ? n_cu : 256, nullptr).bytes;
 }
 

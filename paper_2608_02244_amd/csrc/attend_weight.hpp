@@ -8,9 +8,9 @@
 //   rows kernel   requests with few rows (tokens times query heads per key head): a wave
 //     takes units of 32 keys, all key heads of each, keys straight from the cache into
 //     registers, the next head's under way; bound by the bytes of the keys
-//   tiles kernel  requests with many rows: a block holds 256 keys of a key head in
-//     registers and goes over the rows that see them, which its waves share through LDS;
-//     bound by the products and the exponentials
+//   tiles kernel  requests with many rows: a block holds 256 keys of a key head (128 with
+//     heads of 256) in registers and goes over the rows that see them, which its waves share
+//     through LDS; bound by the products and the exponentials
 // In both the work of all requests forms one line, cut into equal pieces.  The rows kernel's
 // pieces are whole keys, so that a key is one wave's; the tiles kernel's may cut a tile's
 // rows, whose sums are then joined, in their order, by a second launch.  Equal calls give
@@ -423,10 +423,9 @@ struct WeightTileOf {
   static constexpr int LDS = BUFFERS * (BYTES + 256);    // and the line's sums
 };
 
-template <class T, int D, int KIND>
+template <class T, int D, bool FP4>
 __global__ __launch_bounds__(ATT_THREADS, 2) void weight_tiles_kernel(WeightArgs wa,
                                                                       WeightPlan plan) {
-  constexpr bool FP4 = KIND == FP4_PAGES;
   using L = WeightTileOf<D>;
   constexpr int NK = L::GROUPS, KB = L::KEYS, SR = L::ROWS, QC = D / 16, TILES = SR / 32;
   using elem = typename T::elem;

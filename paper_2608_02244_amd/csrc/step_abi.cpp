@@ -280,7 +280,7 @@ int weight_entry(const fsched_attn_params* p, const Cache* kv, const void* q, co
   hipError_t e;
   {
     Workspace ws;
-    rc = ws.take(workspace, workspace_bytes, fs::weight_workspace(a, c.fp4, c.head_dim, n_cu), s);
+    rc = ws.take(workspace, workspace_bytes, fs::weight_workspace(a, c.head_dim, n_cu), s);
     if (rc) return rc;
     e = fs::launch_weight(a, c.fp4, c.dtype, c.head_dim, n_cu, ws.get(), s);
   }
@@ -299,7 +299,7 @@ int weight_bytes(const fsched_attn_params* p, const Cache* kv, int64_t* bytes) {
   fs::WeightArgs a;
   std::memset(&a, 0, sizeof(a));
   a.at = attn_args(p, c);
-  *bytes = (int64_t)fs::weight_workspace(a, c.fp4, c.head_dim, fs::compute_units());
+  *bytes = (int64_t)fs::weight_workspace(a, c.head_dim, fs::compute_units());
   return FSCHED_OK;
 }
 

@@ -117,7 +117,7 @@ size_t attend_workspace(const AttnArgs& a, bool fp4, int head_dim, int n_cu);
 hipError_t launch_attend(const AttnArgs& a, bool fp4, int dtype, int head_dim, int n_cu,
                          void* workspace, hipStream_t s);
 
-size_t weight_workspace(const WeightArgs& a, bool fp4, int head_dim, int n_cu);
+size_t weight_workspace(const WeightArgs& a, int head_dim, int n_cu);
 hipError_t launch_weight(const WeightArgs& a, bool fp4, int dtype, int head_dim, int n_cu,
                          void* workspace, hipStream_t s);
 
