@@ -26,8 +26,8 @@ constexpr int THREADS = 256;
 constexpr int LDS_PAGES = 4096, ALONE_TOKENS = 32768;
 
 struct Scratch {
-  uint64_t* key;   // [n_req][width] scores in an order of whole numbers
-  int32_t* from;   // [n_req][width] old place of each page that stays
+  uint64_t* key;   // [n_req][width] scores in an order of whole numbers (not ALONE)
+  int32_t* from;   // [n_req][width] old place of each page that stays (not ALONE)
   int32_t* gone;   // [n_req][width] ids of the pages given up
   int32_t* freed;  // [n_req] ids in `gone`
 };
@@ -309,8 +309,13 @@ __global__ __launch_bounds__(THREADS) void nothing_kernel(EvictArgs a) {
 
 size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 
+// Whether one block takes each request.
+bool rows_alone(const EvictArgs& a) {
+  return a.width <= LDS_PAGES && (int64_t)a.width << a.page_shift <= ALONE_TOKENS;
+}
+
 Scratch scratch(const EvictArgs& a, char* ws, size_t* bytes) {
-  const size_t cells = (size_t)a.n_req * a.width;
+  const size_t cells = (size_t)a.n_req * a.width, shared = rows_alone(a) ? 0 : cells;
   size_t used = 0;
   auto take = [&](size_t n) {
     char* at = ws ? ws + used : nullptr;
@@ -318,8 +323,8 @@ Scratch scratch(const EvictArgs& a, char* ws, size_t* bytes) {
     return at;
   };
   Scratch w;
-  w.key = (uint64_t*)take(cells * 8);
-  w.from = (int32_t*)take(cells * 4);
+  w.key = (uint64_t*)take(shared * 8);
+  w.from = (int32_t*)take(shared * 4);
   w.gone = (int32_t*)take(cells * 4);
   w.freed = (int32_t*)take((size_t)a.n_req * 4);
   *bytes = used;
@@ -350,7 +355,7 @@ hipError_t launch_evict(const EvictArgs& a, int n_cu, void* workspace, hipStream
   };
   // no launch without the one before: it would read what that one writes
   hipError_t e;
-  if (a.width <= LDS_PAGES && row <= ALONE_TOKENS) {
+  if (rows_alone(a)) {
     select_kernel<512, true><<<a.n_req, 512, 0, s>>>(a, w);
     e = hipGetLastError();
   } else {

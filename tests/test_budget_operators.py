@@ -275,3 +275,16 @@ def test_cache_of_pages_that_every_call_refuses_is_not_made(page):
         fs.kv4_cache(3, 2, page, 64, device="cpu")
     for page in (16, 64, 65536):
         assert fs.kv4_cache(1, 1, page, 64, device="cpu").shape == (1, 1, page // 16, 17 * 64)
+
+
+@pytest.mark.parametrize("page,width,alone", [(16, 200, True), (1, 4096, True), (1, 4097, False),
+                                              (16, 2048, True), (16, 2049, False), (8, 0, True)])
+def test_evict_workspace_is_what_the_call_uses(page, width, alone):
+    """The freed ids (4 bytes a page) and their number; rows that no single block holds have
+    scores and places beside them (12 bytes a page)."""
+    p = step.EvictParams(n_req=500, table_width=width, page_size=page, flags=DEV,
+                         weight_stride=width * page)
+    x = ctypes.c_int64()
+    assert fs.lib().fsched_kv_evict_workspace(ref(p), ref(x)) == fs.OK
+    need = 500 * (width * (4 if alone else 16) + 4)
+    assert need <= x.value < need + 4 * 256
