@@ -487,8 +487,9 @@ int fsched_attend_workspace(const fsched_attn_params* p, const fsched_kv_cache* 
  * Codes are the values' places in that list, 8 added for a negative one; byte i of a
  * token's codes holds elements 2i (low) and 2i + 1; a scale is the byte e + 127, or 255
  * where the 32 elements are not all finite (they then stand for NaN).  e is -125 .. 125
- * in bf16 and -23 .. 13 in f16 (magnitudes above 49,152 are held as that), so that every
- * held value is an element of the type: nothing is rounded a second time.
+ * in bf16 and -23 .. 13 in f16 (magnitudes above 6 times the largest scale, 2.55e38 and
+ * 49,152, are held as that), so that every held value is an element of the type: nothing is
+ * rounded a second time.
  *
  * 16 tokens of one head in a page are a group, 17 head_dim bytes in one piece (all of
  * them together 17/32 of a byte an element, keys and values):
@@ -604,7 +605,9 @@ int fsched_attend4_weight_workspace(const fsched_attn_params* p, const fsched_kv
  *                   then 0.  Neither may overlap its input.
  *   new_len         [n_req]
  *   freed           [n_freed] ids of the pages given up (entries of the table below 0 are
- *                   none), requests in order, pages in order; then -1
+ *                   none), requests in order, pages in order; then -1.  An id stands there
+ *                   once for each entry of the table that gave it up: a page that two
+ *                   requests list may still be another's, or come twice
  *   count           [1] pages given up with an id, also those beyond n_freed
  *   workspace       as for fsched_attend */
 typedef struct {

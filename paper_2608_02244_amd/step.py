@@ -280,7 +280,8 @@ def kv_evict(weight, kv_len, block_table, budget, *, page_size: int, n_sink: int
 
     Returns (block_table, weight, kv_len, freed [n_freed], count [1]), new tensors: tables
     and weights closed up (behind what stays -1 and 0), the ids of the freed pages with -1
-    behind them, and how many there are."""
+    behind them, and how many there are.  A page that several requests list is given up by
+    each of them for itself: its id is there once for each."""
     if stream is not None:
         with _on(stream, weight):
             return kv_evict(weight, kv_len, block_table, budget, page_size=page_size,

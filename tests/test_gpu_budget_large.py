@@ -259,3 +259,14 @@ def test_evict_rows_past_one_block_with_nothing_to_drop(dev):
     check_evict(dev, [33000, 33600], 2100, 16, 10, sinks=10 ** 9, levels=2)
     check_evict(dev, [33000, 33600], 2100, 16, 10, recent=2 ** 31 - 1, n_freed=5, levels=2)
     check_evict(dev, [33000, 33600, 20000], 2100, 16, 0, n_freed=100, rows_apart=1)
+
+
+def test_evict_a_page_that_two_requests_list(dev):
+    """Each request gives it up for itself: its id comes once for each that does."""
+    import torch
+    table = torch.tensor([[5, 6, 7], [5, 8, 9], [5, 2, 3]], dtype=torch.int32, device=dev)
+    weight = torch.tensor([[0.0, 2, 1], [0, 1, 2], [3, 2, 1]], device=dev)
+    kv = torch.tensor([3, 3, 3], dtype=torch.int32, device=dev)
+    got = fs.kv_evict(weight, kv, table, torch.full_like(kv, 2), page_size=1)
+    assert got[0].tolist() == [[6, 7, -1], [8, 9, -1], [5, 2, -1]]
+    assert got[3].tolist()[:3] == [5, 5, 3] and got[4].tolist() == [3]
