@@ -33,6 +33,19 @@ Shape shape_of(const WeightArgs& a, int head_dim, int n_cu, char* ws) {
   return s;
 }
 
+// Row tiles of the rows kernel: one if no request can have more than 16 rows, else two, with
+// fewer blocks per compute unit.  One row tile for all steps and requests of 17 to 32 rows in the
+// tiles kernel / as it is, us, caches of 16 bits and of 4:
+//   drafts of 1 to 4 tokens, 64 requests, 8 heads per key head
+//     heads of 64    40 / 16,  37 / 13
+//     heads of 128   70 / 45,  52 / 28
+//     heads of 256   59 / 44,  45 / 28
+//   chunks of up to 512 tokens beside 43 decoding requests, 4 heads per key head (128: 4, 8)
+//     heads of 64    75 / 76,  65 / 70  (window of 2,048)
+//     heads of 128   89 / 92,  72 / 75;  113 / 117,  97 / 100
+//     heads of 256   76 / 82,  59 / 64
+// (Beside chunks, where the tiles kernel runs anyway, one row tile is faster by 1 to 7 %: a rule
+// for those steps alone would have the tiles kernel's least number of rows follow it.)
 template <class T, int D, int KIND>
 hipError_t launch_kind(const WeightArgs& a, const Shape& p, int n_cu, hipStream_t s) {
   const size_t line = (size_t)(ATT_WAVES + a.at.n_req + 1) * sizeof(int64_t);

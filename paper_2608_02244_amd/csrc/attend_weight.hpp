@@ -17,8 +17,15 @@
 // equal bits.
 //
 // Measured (heads of 128, bf16): 64 requests holding 65,000 tokens, 31 us or 4.3 TB/s; 512
-// holding 0.73 M in 4 bits, 59 us or 3.5 TB/s (4.1 without the start); prompts of 25,600 tokens, 366 us or 820
-// TFLOP/s (beside them 5 us of requests with few rows and 6 of joins).
+// holding 0.73 M in 4 bits, 59 us or 3.5 TB/s (4.1 without the start); prompts of 25,600
+// tokens, calls of 360 to 381 us on the cards that it ran on, 6 of them the joins and 5 a rows
+// kernel that finds no request (the tiles alone 366 us or 820 TFLOP/s, traced on a card whose
+// calls took 381); over 4 bits 350 us.
+//
+// Sums are of 32 bits.  A lane of the tiles kernel adds a key's terms one after the other, some
+// 2,500 in those prompts, which errs by a root of their number: the weights are 1.6e-7 (of their
+// norm) from 64 bits, and 8.7e-8 where terms are added pairwise.  Of decode steps both are
+// 2.9e-8.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -423,6 +430,13 @@ struct WeightTileOf {
   static constexpr int LDS = BUFFERS * (BYTES + 256);    // and the line's sums
 };
 
+// Registers: heads of 128 take all 256 and spill 22 (26 over 4 bits).  Those are the thread's
+// rows of a stage, which `fetch` reads back, each behind a wait for all loads, where it makes the
+// offsets anew: at a tile's start and end, and in every stage where 64 is no multiple of the
+// group.  The stages under way are waited for with them: prompts with 5 query heads to a key
+// head take 493 us, 10 % more for each product than with 4.  Counted in the prompts with 4:
+// vector instructions issue in 54 % of the cycles, the matrix units are busy in 36 %, and 1.6 of
+// 2 waves are there.
 template <class T, int D, bool FP4>
 __global__ __launch_bounds__(ATT_THREADS, 2) void weight_tiles_kernel(WeightArgs wa,
                                                                       WeightPlan plan) {
